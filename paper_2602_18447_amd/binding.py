@@ -43,6 +43,11 @@ class KV(C.Structure):
                 ("block_size", C.c_int32), ("block_table", C.c_void_p), ("max_blocks_per_seq", C.c_int32)]
 
 
+class KV4(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("n_blocks", C.c_int32), ("block_size", C.c_int32), ("block_table", C.c_void_p),
+                ("max_blocks_per_seq", C.c_int32)]
+
+
 class Batch(C.Structure):
     _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("suffix_ids", C.c_void_p), ("cu_suffix", C.c_void_p),
                 ("prefix_lens", C.c_void_p), ("h_cu_suffix", C.POINTER(C.c_int32)),
@@ -131,6 +136,20 @@ def _load() -> C.CDLL:
                                            vp, sz, vp, vp, vp, vp, vp]
     lib.confspec_op_workspace_slices.restype = C.c_int
     lib.confspec_op_workspace_slices.argtypes = [vp, i32, i32, P(Batch), P(sz), P(sz), P(i32), P(sz)]
+    lib.confspec_op_kv4_append.restype = C.c_int
+    lib.confspec_op_kv4_append.argtypes = [vp, P(KV4), P(Batch), i32, vp, C.c_int64, vp, P(i32), vp, vp, vp, vp]
+    lib.confspec_op_kv4_read.restype = C.c_int
+    lib.confspec_op_kv4_read.argtypes = [vp, P(KV4), P(Batch), i32, vp, vp, vp]
+    lib.confspec_op_kv4_attention.restype = C.c_int
+    lib.confspec_op_kv4_attention.argtypes = [vp, P(KV4), P(Batch), i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.confspec_op_kv4_attention_scratch_bytes.restype = C.c_int
+    lib.confspec_op_kv4_attention_scratch_bytes.argtypes = [vp, P(Batch), P(sz)]
+    lib.confspec_w4_bytes.restype = sz
+    lib.confspec_w4_bytes.argtypes = [i32, i32, i32]
+    lib.confspec_w4_pack.restype = C.c_int
+    lib.confspec_w4_pack.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]
+    lib.confspec_op_w4_gemm.restype = C.c_int
+    lib.confspec_op_w4_gemm.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]
     lib.confspec_phase_timing.restype = C.c_int
     lib.confspec_phase_timing.argtypes = [vp, i32]
     lib.confspec_phase_times.restype = C.c_int
@@ -147,7 +166,9 @@ EXPORTED = ["confspec_version", "confspec_create", "confspec_destroy", "confspec
             "confspec_op_gemm", "confspec_op_gemm_scratch_bytes", "confspec_op_rmsnorm", "confspec_op_rope_split", "confspec_op_qkv_rope", "confspec_op_attention",
             "confspec_op_verdict_gate", "confspec_tune", "confspec_cascade_scratch_bytes",
             "confspec_cascade", "confspec_verify_append", "confspec_head_scratch_bytes", "confspec_generate_step",
-            "confspec_static_scratch_need", "confspec_verify_static", "confspec_phase_timing", "confspec_phase_times", "confspec_verify_shared", "confspec_op_workspace_slices"]
+            "confspec_static_scratch_need", "confspec_verify_static", "confspec_phase_timing", "confspec_phase_times", "confspec_verify_shared", "confspec_op_workspace_slices",
+            "confspec_op_kv4_append", "confspec_op_kv4_read", "confspec_op_kv4_attention", "confspec_op_kv4_attention_scratch_bytes",
+            "confspec_w4_bytes", "confspec_w4_pack", "confspec_op_w4_gemm"]
 
 
 class ConfSpecError(RuntimeError):
@@ -341,6 +362,52 @@ def confspec_op_verdict_gate(ctx, batch: Batch, x, final_norm, lm_head, verdict_
                                              _ptr(verdict), _ptr(accept), _stream_handle(stream)))
 
 
+# 4-bit weights and cache (include/confspec_int4.h)
+W4_MAX_ROWS = 128
+KV4_PAGE_BYTES = 2176
+
+
+def confspec_op_kv4_append(ctx, kv: KV4, batch: Batch, layer: int, qkv, n_append, h_n_append, q, k, v, qkv_stride: Optional[int] = None,
+                           stream=None) -> None:
+    """qkv: fp32 rows of qkv_stride elements (default: the tensor's row stride).  n_append / h_n_append: device tensor and
+    host int32 array, or both None (every token)."""
+    import numpy as np
+    hn = None if h_n_append is None else np.ascontiguousarray(h_n_append, dtype=np.int32)
+    hp = None if hn is None else hn.ctypes.data_as(C.POINTER(C.c_int32))
+    _check(ctx, lib.confspec_op_kv4_append(ctx, C.byref(kv), C.byref(batch), layer, _ptr(qkv),
+                                           qkv.stride(0) if qkv_stride is None else qkv_stride, _ptr(n_append), hp, _ptr(q),
+                                           _ptr(k), _ptr(v), _stream_handle(stream)))
+
+
+def confspec_op_kv4_read(ctx, kv: KV4, batch: Batch, layer: int, k, v, stream=None) -> None:
+    _check(ctx, lib.confspec_op_kv4_read(ctx, C.byref(kv), C.byref(batch), layer, _ptr(k), _ptr(v), _stream_handle(stream)))
+
+
+def confspec_op_kv4_attention_scratch_bytes(ctx, batch: Batch) -> int:
+    out = C.c_size_t()
+    _check(ctx, lib.confspec_op_kv4_attention_scratch_bytes(ctx, C.byref(batch), C.byref(out)))
+    return out.value
+
+
+def confspec_op_kv4_attention(ctx, kv: KV4, batch: Batch, layer: int, q, k_suffix, v_suffix, out, scratch, stream=None) -> None:
+    _check(ctx, lib.confspec_op_kv4_attention(ctx, C.byref(kv), C.byref(batch), layer, _ptr(q), _ptr(k_suffix), _ptr(v_suffix),
+                                              _ptr(out), _ptr(scratch), _nbytes(scratch), _stream_handle(stream)))
+
+
+def confspec_w4_bytes(N: int, K: int, group: int) -> int:
+    return int(lib.confspec_w4_bytes(N, K, group))
+
+
+def confspec_w4_pack(ctx, codes, scales, zeros, N: int, K: int, group: int, dst, gate_up: bool = False, stream=None) -> None:
+    _check(ctx, lib.confspec_w4_pack(ctx, _ptr(codes), _ptr(scales), _ptr(zeros), N, K, group, 1 if gate_up else 0, _ptr(dst),
+                                     _nbytes(dst), _stream_handle(stream)))
+
+
+def confspec_op_w4_gemm(ctx, A, W4, residual, out, M: int, N: int, K: int, group: int, epilogue: int, stream=None) -> None:
+    _check(ctx, lib.confspec_op_w4_gemm(ctx, _ptr(A), _ptr(W4), _ptr(residual), _ptr(out), M, N, K, group, epilogue,
+                                        _stream_handle(stream)))
+
+
 def confspec_cascade_scratch_bytes(max_B: int, max_T: int, max_blocks_per_seq_target: int) -> int:
     return int(lib.confspec_cascade_scratch_bytes(max_B, max_T, max_blocks_per_seq_target))
 
@@ -422,6 +489,10 @@ def make_weights(embed, lm_head, final_norm, attn_norm, wqkv, wo, mlp_norm, w_ga
 
 def make_kv(k_pages, v_pages, block_table, n_blocks: int, block_size: int, max_blocks_per_seq: int) -> KV:
     return KV(_ptr(k_pages), _ptr(v_pages), n_blocks, block_size, _ptr(block_table), max_blocks_per_seq)
+
+
+def make_kv4(pages, block_table, n_blocks: int, block_size: int, max_blocks_per_seq: int) -> KV4:
+    return KV4(_ptr(pages), n_blocks, block_size, _ptr(block_table), max_blocks_per_seq)
 
 
 def make_batch(suffix_ids, cu_suffix, prefix_lens, h_cu_suffix, h_prefix_lens):

@@ -18,6 +18,7 @@
 #include "../../include/confspec_append.h"
 #include "../../include/confspec_generate.h"
 #include "../../include/confspec_static.h"
+#include "../../include/confspec_int4.h"
 #include "kernels.h"
 
 // Scratch of confspec_verify_static: one array per GPU, part of the loaded code object, held until the process ends.
@@ -1304,6 +1305,157 @@ int confspec_op_verdict_gate(confspec_ctx *ctx, const confspec_batch *batch, con
     HIP_TRY(cs::launch_verdict(c.dtype, dev_x, (const int32_t *)(ws + L.last_row), dev_final_norm, dev_lm_head, va,
                                batch->B, batch->T, c.d_model, c.rms_eps, dev_verdict_logits, dev_conf, dev_verdict,
                                dev_accept, s));
+    return CONFSPEC_OK;
+}
+
+// ---- 4-bit weights and cache (confspec_int4.h) ----
+
+namespace {
+int check_int4_ctx(const confspec_ctx *ctx) {
+    if (ctx->cfg.dtype != CONFSPEC_DTYPE_BF16) return fail(ctx, CONFSPEC_E_UNSUPPORTED, "4-bit operators need a bf16 context");
+    return CONFSPEC_OK;
+}
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// Checks cache, layer and batch; rows (may be null: the context alone has to fit) = rows behind each context that are touched.
+int check_kv4(const confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_batch *batch, int32_t layer, bool touch_suffix,
+              const int32_t *h_rows, cs::Kv4Batch *out) {
+    const confspec_model_cfg &c = ctx->cfg;
+    int rc;
+    if ((rc = check_int4_ctx(ctx))) return rc;
+    if (!kv) return fail(ctx, CONFSPEC_E_INVALID_ARG, "kv is null");
+    if (kv->max_blocks_per_seq < 1 || kv->n_blocks < 1) return fail(ctx, CONFSPEC_E_INVALID_ARG, "kv: max_blocks_per_seq and n_blocks must be >= 1");
+    if (kv->block_size != 16) return fail(ctx, CONFSPEC_E_UNSUPPORTED, "a 4-bit cache has block_size 16 (got %d)", kv->block_size);
+    if (!kv->block_table || !kv->pages) return fail(ctx, CONFSPEC_E_INVALID_ARG, "kv: pages or block_table is null");
+    if (!aligned16(kv->pages)) return fail(ctx, CONFSPEC_E_INVALID_ARG, "kv pages must be 16-byte aligned");
+    if (layer < 0 || layer >= (c.n_layers > 0 ? c.n_layers : 1)) return fail(ctx, CONFSPEC_E_INVALID_ARG, "layer %d out of range", layer);
+    const int64_t cap = (int64_t)kv->max_blocks_per_seq * 16;
+    if ((rc = check_batch(ctx, batch, cap, nullptr))) return rc;
+    for (int b = 0; b < batch->B; ++b) {
+        const int S = batch->h_cu_suffix[b + 1] - batch->h_cu_suffix[b], L = batch->h_prefix_lens[b];
+        if ((int64_t)L + S > INT32_MAX - 4096) return fail(ctx, CONFSPEC_E_OUT_OF_RANGE, "trace %d ends at position %lld", b, (long long)L + S);
+        if (!touch_suffix) continue;
+        const int n = h_rows ? h_rows[b] : S;
+        if (n < 0 || n > S) return fail(ctx, CONFSPEC_E_OUT_OF_RANGE, "n_append[%d] = %d outside [0, S_b = %d]", b, n, S);
+        if ((int64_t)L + n > cap)
+            return fail(ctx, CONFSPEC_E_OUT_OF_RANGE, "trace %d: rows up to %lld, block table capacity %lld", b, (long long)L + n, (long long)cap);
+    }
+    *out = cs::Kv4Batch{batch->cu_suffix, batch->prefix_lens, kv->block_table,
+                        (uint8_t *)kv->pages + (size_t)layer * kv->n_blocks * c.n_kv_heads * cs::KV4_PAGE,
+                        batch->B, batch->T, c.n_kv_heads, kv->n_blocks, kv->max_blocks_per_seq};
+    return CONFSPEC_OK;
+}
+}  // namespace
+
+int confspec_op_kv4_append(confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_batch *batch, int32_t layer,
+                           const float *dev_qkv, int64_t qkv_stride, const int32_t *dev_n_append, const int32_t *h_n_append,
+                           void *dev_q, void *dev_k, void *dev_v, confspec_stream stream) {
+    if (!ctx) return CONFSPEC_E_INVALID_ARG;
+    if (!dev_qkv || !dev_q || !dev_k || !dev_v) return fail(ctx, CONFSPEC_E_INVALID_ARG, "null operand");
+    if ((dev_n_append == nullptr) != (h_n_append == nullptr))
+        return fail(ctx, CONFSPEC_E_INVALID_ARG, "dev_n_append and h_n_append must both be given or both be null");
+    cs::Kv4Append a = {};
+    int rc;
+    if ((rc = check_kv4(ctx, kv, batch, layer, true, h_n_append, &a.b))) return rc;
+    const confspec_model_cfg &c = ctx->cfg;
+    if (!aligned16(dev_qkv) || !aligned16(dev_q) || !aligned16(dev_k) || !aligned16(dev_v))
+        return fail(ctx, CONFSPEC_E_INVALID_ARG, "operands must be 16-byte aligned");
+    if (qkv_stride < ((int64_t)c.n_q_heads + 2 * (int64_t)c.n_kv_heads) * 128 || qkv_stride % 4)
+        return fail(ctx, CONFSPEC_E_INVALID_ARG, "qkv_stride = %lld: a multiple of 4, at least (Hq + 2 Hkv) * 128", (long long)qkv_stride);
+    a.qkv = dev_qkv;
+    a.stride = qkv_stride;
+    a.n_append = dev_n_append;
+    a.q = (cs::bf16 *)dev_q; a.k = (cs::bf16 *)dev_k; a.v = (cs::bf16 *)dev_v;
+    a.Hq = c.n_q_heads;
+    for (int i = 0; i < 64; ++i) a.inv_freq[i] = std::pow((double)c.rope_theta, -2.0 * i / 128.0);
+    if ((rc = check_device(ctx))) return rc;
+    HIP_TRY(cs::launch_kv4_append(a, (hipStream_t)stream));
+    return CONFSPEC_OK;
+}
+
+int confspec_op_kv4_read(confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_batch *batch, int32_t layer, float *dev_k,
+                         float *dev_v, confspec_stream stream) {
+    if (!ctx) return CONFSPEC_E_INVALID_ARG;
+    if (!dev_k || !dev_v) return fail(ctx, CONFSPEC_E_INVALID_ARG, "null operand");
+    cs::Kv4Batch b;
+    int rc;
+    if ((rc = check_kv4(ctx, kv, batch, layer, true, nullptr, &b))) return rc;
+    if (!aligned16(dev_k) || !aligned16(dev_v)) return fail(ctx, CONFSPEC_E_INVALID_ARG, "operands must be 16-byte aligned");
+    if ((rc = check_device(ctx))) return rc;
+    HIP_TRY(cs::launch_kv4_read(b, dev_k, dev_v, (hipStream_t)stream));
+    return CONFSPEC_OK;
+}
+
+int confspec_op_kv4_attention_scratch_bytes(const confspec_ctx *ctx, const confspec_batch *batch, size_t *out_bytes) {
+    if (!ctx || !out_bytes) return CONFSPEC_E_INVALID_ARG;
+    int rc;
+    if ((rc = check_int4_ctx(ctx)) || (rc = check_batch(ctx, batch, INT32_MAX, nullptr))) return rc;
+    *out_bytes = cs::kv4_attn_scratch(batch->h_cu_suffix, batch->h_prefix_lens, batch->B, ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads);
+    return CONFSPEC_OK;
+}
+
+int confspec_op_kv4_attention(confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_batch *batch, int32_t layer,
+                              const void *dev_q, const void *dev_k_suffix, const void *dev_v_suffix, void *dev_out,
+                              void *dev_scratch, size_t scratch_bytes, confspec_stream stream) {
+    if (!ctx) return CONFSPEC_E_INVALID_ARG;
+    if (!dev_q || !dev_k_suffix || !dev_v_suffix || !dev_out) return fail(ctx, CONFSPEC_E_INVALID_ARG, "null operand");
+    cs::Kv4Attn a = {};
+    int rc;
+    if ((rc = check_kv4(ctx, kv, batch, layer, false, nullptr, &a.b))) return rc;
+    if (!aligned16(dev_q) || !aligned16(dev_k_suffix) || !aligned16(dev_v_suffix) || !aligned16(dev_out))
+        return fail(ctx, CONFSPEC_E_INVALID_ARG, "operands must be 16-byte aligned");
+    const size_t need = cs::kv4_attn_scratch(batch->h_cu_suffix, batch->h_prefix_lens, batch->B, ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads);
+    if (need && (rc = check_ws(ctx, dev_scratch, scratch_bytes, need))) return rc;
+    a.q = (const cs::bf16 *)dev_q; a.k = (const cs::bf16 *)dev_k_suffix; a.v = (const cs::bf16 *)dev_v_suffix;
+    a.out = (cs::bf16 *)dev_out;
+    a.Hq = ctx->cfg.n_q_heads;
+    if ((rc = check_device(ctx))) return rc;
+    HIP_TRY(cs::launch_kv4_attn(a, batch->h_cu_suffix, batch->h_prefix_lens, dev_scratch, (hipStream_t)stream));
+    return CONFSPEC_OK;
+}
+
+size_t confspec_w4_bytes(int32_t N, int32_t K, int32_t group) {
+    if (N < 16 || N % 16 || K < 1 || (group != 32 && group != 64 && group != 128) || K % group) return 0;
+    return (size_t)(N / 16) * cs::w4_kblocks(K) * cs::w4_record(group);
+}
+
+int confspec_w4_pack(confspec_ctx *ctx, const void *dev_codes, const void *dev_scales, const void *dev_zeros, int32_t N,
+                     int32_t K, int32_t group, int32_t gate_up, void *dev_dst, size_t dst_bytes, confspec_stream stream) {
+    if (!ctx) return CONFSPEC_E_INVALID_ARG;
+    int rc;
+    if ((rc = check_int4_ctx(ctx))) return rc;
+    if (!dev_codes || !dev_scales) return fail(ctx, CONFSPEC_E_INVALID_ARG, "null operand");
+    if (gate_up != 0 && gate_up != 1) return fail(ctx, CONFSPEC_E_INVALID_ARG, "gate_up must be 0 or 1");
+    const size_t need = confspec_w4_bytes(N, K, group);
+    if (!need) return fail(ctx, CONFSPEC_E_UNSUPPORTED, "4-bit weights: N %% 16 == 0, group 32, 64 or 128, K %% group == 0 (N = %d, K = %d, group = %d)", N, K, group);
+    if (((uintptr_t)dev_codes & 3) || ((uintptr_t)dev_scales & 1) || ((uintptr_t)dev_zeros & 1))
+        return fail(ctx, CONFSPEC_E_INVALID_ARG, "codes must be 4-byte aligned, scales and zeros 2-byte aligned");
+    if (!dev_dst || ((uintptr_t)dev_dst & 255)) return fail(ctx, CONFSPEC_E_WORKSPACE, "dev_dst null or not 256-byte aligned");
+    if (dst_bytes < need) return fail(ctx, CONFSPEC_E_WORKSPACE, "dev_dst has %zu bytes, %zu needed", dst_bytes, need);
+    if ((rc = check_device(ctx))) return rc;
+    HIP_TRY(cs::launch_w4_pack((const uint8_t *)dev_codes, (const __half *)dev_scales, (const __half *)dev_zeros, (uint8_t *)dev_dst, N, K,
+                               group, gate_up, (hipStream_t)stream));
+    return CONFSPEC_OK;
+}
+
+int confspec_op_w4_gemm(confspec_ctx *ctx, const void *dev_A, const void *dev_W4, const float *dev_residual, void *dev_out,
+                        int32_t M, int32_t N, int32_t K, int32_t group, int32_t epilogue, confspec_stream stream) {
+    if (!ctx) return CONFSPEC_E_INVALID_ARG;
+    int rc;
+    if ((rc = check_int4_ctx(ctx))) return rc;
+    if (!dev_A || !dev_W4 || !dev_out) return fail(ctx, CONFSPEC_E_INVALID_ARG, "null operand");
+    if (!aligned16(dev_A) || !aligned16(dev_out) || !aligned16(dev_residual) || ((uintptr_t)dev_W4 & 255))
+        return fail(ctx, CONFSPEC_E_INVALID_ARG, "operands must be 16-byte aligned, packed weights 256-byte aligned");
+    if (epilogue < 0 || epilogue > 2) return fail(ctx, CONFSPEC_E_INVALID_ARG, "unknown epilogue %d", epilogue);
+    if ((epilogue == CONFSPEC_EPI_RESID_F32) != (dev_residual != nullptr))
+        return fail(ctx, CONFSPEC_E_INVALID_ARG, "dev_residual goes with the residual epilogue, and only with it");
+    if (M < 1) return fail(ctx, CONFSPEC_E_INVALID_ARG, "M = %d", M);
+    if (M > CONFSPEC_W4_MAX_ROWS) return fail(ctx, CONFSPEC_E_UNSUPPORTED, "M = %d: products with 4-bit weights take at most %d rows", M, CONFSPEC_W4_MAX_ROWS);
+    if (!confspec_w4_bytes(N, K, group))
+        return fail(ctx, CONFSPEC_E_UNSUPPORTED, "4-bit weights: N %% 16 == 0, group 32, 64 or 128, K %% group == 0 (N = %d, K = %d, group = %d)", N, K, group);
+    if ((rc = check_device(ctx))) return rc;
+    HIP_TRY(cs::launch_w4_gemm(cs::W4Gemm{(const cs::bf16 *)dev_A, (const uint8_t *)dev_W4, dev_residual, dev_out, M, N, K, group, epilogue},
+                               (hipStream_t)stream));
     return CONFSPEC_OK;
 }
 

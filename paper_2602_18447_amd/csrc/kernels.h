@@ -325,6 +325,50 @@ int few_attn_rows(bool one);
 void few_attn_pieces(FewAttn &a, bool one);      // from n_tiles, Hkv and max_L: pieces, wave_pages, fold
 hipError_t launch_few_attn(FewAttn a, hipStream_t s);
 
+// ---- cache in 4 bits (kv4.hip): page format in confspec_int4.h ----
+constexpr int KV4_PAGE = 2176, KV4_V = 1024, KV4_KP = 2048, KV4_VP = 2112;   // a page's bytes; offsets of its other parts
+// Batch and cache of one layer as the kernels see them; indexes are clamped on the device.
+struct Kv4Batch {
+    const int32_t *cu, *plens, *table;
+    uint8_t *pages;           // this layer's pages [n_blocks, Hkv, KV4_PAGE]
+    int32_t B, T, Hkv, n_blocks, max_blocks;
+};
+struct Kv4Append {
+    Kv4Batch b;
+    const float *qkv;
+    int64_t stride;
+    const int32_t *n_append;  // null: all tokens
+    bf16 *q, *k, *v;
+    int32_t Hq;
+    double inv_freq[64];
+};
+hipError_t launch_kv4_append(const Kv4Append &a, hipStream_t s);
+hipError_t launch_kv4_read(const Kv4Batch &b, float *k, float *v, hipStream_t s);
+struct Kv4Attn {
+    Kv4Batch b;
+    const bf16 *q, *k, *v;    // [T, Hq, 128], suffix [T, Hkv, 128]
+    bf16 *out;
+    int32_t Hq;
+};
+size_t kv4_attn_scratch(const int32_t *h_cu, const int32_t *h_lens, int B, int Hq, int Hkv);
+hipError_t launch_kv4_attn(const Kv4Attn &a, const int32_t *h_cu, const int32_t *h_lens, void *scratch, hipStream_t s);
+
+// ---- products with 4-bit weights (w4.hip) ----
+// Records of 16 rows x 128 k: [N / 16][ceil(K / 128)] of the key codes' layout (row for token) and 128 / group x 16 pairs (s, z).
+constexpr int W4_MAX_ROWS = 128;
+__host__ __device__ inline int w4_record(int group) { return 1024 + 64 * (128 / group); }
+__host__ __device__ inline int w4_kblocks(int K) { return (K + 127) / 128; }
+hipError_t launch_w4_pack(const uint8_t *codes, const __half *scales, const __half *zeros, uint8_t *dst, int N, int K, int group,
+                          int gate_up, hipStream_t s);
+struct W4Gemm {
+    const bf16 *A;            // [M, K]
+    const uint8_t *W;
+    const float *resid;
+    void *out;
+    int32_t M, N, K, group, epi;
+};
+hipError_t launch_w4_gemm(const W4Gemm &a, hipStream_t s);
+
 // ---- cascade (cascade.hip) ----
 hipError_t launch_cascade_select(const uint8_t *keep, const int32_t *verdict_d, const int32_t *req_start, const int32_t *parent,
                                  int R, int B, const int32_t *cu, const int32_t *plens, int T, uint8_t *open_flag,
