@@ -28,7 +28,7 @@ extern "C" {
  * A cache row is one token of one kv head, 128 elements.  It stands for the values z + s * c: codes c in 0..15 and, per row,
  * two IEEE halves s and z.  A row x (bf16 values, clamped to +-65504) is stored as
  *     z = half(min x),  s = half(fp32((max x - z) / 15)),  c = (x - z) / s to the nearest whole number, ties to even,
- *     within 0..15 (0 where s is 0); a zero z is +0.
+ *     within 0..15 (0 where s is 0); a zero s or z is +0.
  * A NaN among the elements is stored as some number of the row's range.
  * Keys are stored rotated.  A page holds 16 tokens of one head, keys and values:
  *   byte    0  key codes: 32-bit word ((c * 16 + token) * 4 + i) has elements d = 32 i + 8 c + e, e = 0..7, the even

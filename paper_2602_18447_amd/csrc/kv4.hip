@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a) {
         for (int o = 32; o > 0; o >>= 1) { mn = fminf(mn, __shfl_xor(mn, o, 64)); mx = fmaxf(mx, __shfl_xor(mx, o, 64)); }
         const __half zh = __float2half_rn(mn + 0.f);            // (never -0)
         const float z = __half2float(zh);
-        const __half sh = __float2half_rn((float)(((double)mx - (double)z) / 15.0));
+        const __half sh = __float2half_rn((float)(((double)mx - (double)z) / 15.0) + 0.f);
         const float s = __half2float(sh);
         const float c0 = s > 0.f ? fminf(fmaxf(rintf((x0 - z) / s), 0.f), 15.f) : 0.f;
         const float c1 = s > 0.f ? fminf(fmaxf(rintf((x1 - z) / s), 0.f), 15.f) : 0.f;
@@ -129,68 +129,521 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, float *__rest
     }
 }
 
-// One wavefront per (token, q head); 64 keys a round, a lane per key for the scores and per two elements for the sums.
-__global__ __launch_bounds__(64) void kv4_attn_kernel(Kv4Attn a) {
-    const Kv4Batch &b = a.b;
-    __shared__ float sq[128], sp[64];
-    const int lane = threadIdx.x, t = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, hk = h / (a.Hq / b.Hkv);
-    const int trace = trace_of(b.cu, b.B, t), t0 = b.cu[trace];
-    const int L = min(max(b.plens[trace], 0), b.max_blocks * 16), n = L + min(max(t - t0, 0), b.T - 1) + 1;
-    const bf16 *q = a.q + ((size_t)t * a.Hq + h) * 128;
-    sq[lane] = bf16_f32(q[lane]) * 0.08838834764831845f;
-    sq[lane + 64] = bf16_f32(q[lane + 64]) * 0.08838834764831845f;
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int j0 = 0; j0 < n; j0 += 64) {
-        const int j = j0 + lane;
-        float s = -INFINITY;
-        if (j < n) {
-            s = 0.f;
-            if (j < L) {
-                const uint8_t *page = page_of(b, trace, j, hk);
-                const unsigned p = *(const unsigned *)(page + KV4_KP + (j & 15) * 4);
-                float sum = 0.f;
-                for (int d = 0; d < 128; d += 8) {
-                    const unsigned w = *(const unsigned *)(page + k_word(j & 15, d));
+// ---- attention ----
+//
+// A wavefront takes 16 NQ query rows of one (trace, kv head) - row = token * G + q head - and walks its share of the keys in
+// chunks of 32 tokens: two pages of the cache, then 32 tokens of the suffix at a time.  It shares nothing with other
+// wavefronts until the end and keeps its own (maximum, sum, O).
+//  * Scores S^T = K Q^T: a page's key codes are the first operand of four 16x16x32 products as they lie in memory, 16
+//    bytes a lane; code c enters as the bfloat16 16 + c (the code's four bits put into the mantissa of 16), which is
+//    exact, and the sum starts at -24 sum(q), so that it ends as sum q (c - 8).  A lane then has four keys of one query row:
+//    score = s sum + (z + 8 s) sum(q).
+//  * O^T = V^T P^T: the lane's four keys of both pages are the eight consecutive k of the second operand as they are, and
+//    a page's value codes lie in memory such that a lane's 16 bytes are those four tokens of eight columns.  Code c
+//    enters as the half c 2^-24 (its four bits alone), the probability as the half p s; z is added to the row's sum.
+//    The lane has 32 columns of its one query row, so scaling, sums and output need nothing of other lanes.
+//  * The running reference M of a row is a bound of score + exponent of s (p s is what must fit a half); it is raised,
+//    and what was summed scaled, only where a row goes beyond it by more than 2^8.
+//
+// Bound by the cache's bytes when rows are few (136 bytes a token and head), by the vector pipe when they are many.
+constexpr int ATT_TRACES = 256;       // traces of one launch: its plan travels in the kernel's arguments
+struct AttnPlan4 {
+    int32_t b0, n_items, n_merge_rows, swizzle;
+    uint32_t start[ATT_TRACES + 1];   // first item of a trace
+    uint32_t part[ATT_TRACES];        // first partial record of a trace (cut into pieces[] > 1)
+    uint32_t mrow[ATT_TRACES + 1];    // first (head, row) of a trace for the merge
+    uint16_t pieces[ATT_TRACES];
+};
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ unsigned lo_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }   // b.lo : a.lo
+__device__ __forceinline__ unsigned hi_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+// Eight key codes as bfloat16 16 + c: element 2 k and 2 k + 1 are nibbles k and k + 4.
+__device__ __forceinline__ bf16x8 key_codes(unsigned w) {
+    constexpr unsigned M = 0x00780078u, C = 0x41804180u;
+    const u32x4 r = {((w << 3) & M) | C, ((w >> 1) & M) | C, ((w >> 5) & M) | C, ((w >> 9) & M) | C};
+    return __builtin_bit_cast(bf16x8, r);
+}
+__device__ __forceinline__ unsigned pack_f16(float a, float b) {
+    const f32x2 v = {a, b};
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(v, f16x2));
+}
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+    const f32x2 v = {a, b};
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+}
+__device__ __forceinline__ float max_over_g(float v) {       // over lanes l, l ^ 16, l ^ 32, l ^ 48
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float sum_over_g(float v) {
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+constexpr float SCALE_LOG2 = 0.08838834764831845f * 1.4426950408889634f;
+constexpr float M_NONE = -1e30f;      // reference of a row that has seen no key
+constexpr float M_ROOM = 8.f;         // p s may exceed 2^5 by this power of two: below 2^14, a half ends at 2^16
+constexpr float V_UNIT = 1.f / 16777216.f;
+
+// What a wavefront needs of two pages; a lane's part of the pairs (s, z) are those of its four keys.
+struct Chunk4 {
+    u32x4 k[2], v[2], kp[2], vp[2];
+};
+
+template <int NQ>
+struct Rows4 {                        // state of a wavefront's rows: a lane has row lane % 16 of each 16
+    bf16x8 q[NQ][4];
+    f32x4 q_off[NQ];                  // -24 sum(q), four times
+    float q_sum[NQ], m[NQ], l[NQ], zs[NQ];
+    f32x4 o[NQ][8];                   // [j][r]: column 32 (lane / 16) + 8 r + j, in units of 2^-24
+};
+
+// Raises the references where needed; t_max: the lane's largest score + exponent.
+template <int NQ>
+__device__ __forceinline__ void raise(Rows4<NQ> &R, const float (&t_max)[NQ]) {
+    bool over = false;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { s += sq[d + e] * (float)((w >> k_shift(e)) & 15); sum += sq[d + e]; }
-                }
-                s = param_s(p) * s + param_z(p) * sum;
-            } else {
-                const bf16 *k = a.k + ((size_t)(t0 + j - L) * b.Hkv + hk) * 128;
-                for (int d = 0; d < 128; ++d) s += sq[d] * bf16_f32(k[d]);
-            }
-        }
-        float mx = s;
+    for (int i = 0; i < NQ; ++i) over |= t_max[i] > R.m[i] + M_ROOM;
+    if (!__any(over)) return;
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-        const float mn = fmaxf(m, mx), keep = expf(m - mn);
-        m = mn;
-        sp[lane] = expf(s - m);
-        __syncthreads();
-        o0 *= keep; o1 *= keep; l *= keep;
-        for (int i = 0; i < min(64, n - j0); ++i) {
-            const int jj = j0 + i;
-            const float p = sp[i];
-            l += p;
-            if (jj < L) {
-                const uint8_t *page = page_of(b, trace, jj, hk);
-                const unsigned pr = *(const unsigned *)(page + KV4_VP + (jj & 15) * 4);
-                const unsigned w = *(const unsigned *)(page + v_word(jj & 15, 2 * lane & ~7));
-                const int sh = 4 * (2 * lane & 7);
-                o0 += p * fmaf(param_s(pr), (float)((w >> sh) & 15), param_z(pr));
-                o1 += p * fmaf(param_s(pr), (float)((w >> (sh + 4)) & 15), param_z(pr));
-            } else {
-                const bf16 *v = a.v + ((size_t)(t0 + jj - L) * b.Hkv + hk) * 128;
-                o0 += p * bf16_f32(v[2 * lane]);
-                o1 += p * bf16_f32(v[2 * lane + 1]);
-            }
-        }
-        __syncthreads();
+    for (int i = 0; i < NQ; ++i) {
+        const float m = fmaxf(R.m[i], max_over_g(t_max[i])), f = __builtin_amdgcn_exp2f(R.m[i] - m);
+        R.m[i] = m;
+        R.l[i] *= f;
+        R.zs[i] *= f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) R.o[i][j] *= f;
     }
-    bf16 *out = a.out + ((size_t)t * a.Hq + h) * 128;
-    out[2 * lane] = __float2bfloat16(o0 / l);
-    out[2 * lane + 1] = __float2bfloat16(o1 / l);
+}
+
+// 32 cached tokens, of which the first n_valid count.
+template <int NQ>
+__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g) {
+    f32x4 sc[NQ][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bf16x8 a = key_codes(c.k[x][i]);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) sc[n][x] = mma(a, R.q[n][i], i == 0 ? R.q_off[n] : sc[n][x]);
+        }
+    float vs[2][4], vz[2][4], t_max[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) t_max[n] = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float ks = param_s(c.kp[x][r]) * SCALE_LOG2, kz = param_z(c.kp[x][r]) * SCALE_LOG2;
+            vs[x][r] = param_s(c.vp[x][r]);
+            vz[x][r] = param_z(c.vp[x][r]);
+            const bool valid = 16 * x + 4 * g + r < n_valid;
+            if (n_valid < 32 && !valid) vs[x][r] = vz[x][r] = 0.f;
+            const float e = (float)max((__float_as_uint(vs[x][r]) >> 23) & 255u, 103u);     // exponent of s, biased by 127; of 2^-24 at least
+            kz = fmaf(8.f, ks, kz);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                float s = fmaf(ks, sc[n][x][r], kz * R.q_sum[n]);
+                if (n_valid < 32) s = valid ? s : -INFINITY;
+                sc[n][x][r] = s;
+                t_max[n] = fmaxf(t_max[n], s + e);
+            }
+        }
+    raise<NQ>(R, t_max);
+    f16x8 w[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const float ref = R.m[n] - 132.f;
+        u32x4 pk;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(sc[n][x][r] - ref), p1 = __builtin_amdgcn_exp2f(sc[n][x][r + 1] - ref);
+                R.l[n] += p0;
+                R.l[n] += p1;
+                R.zs[n] = fmaf(p0, vz[x][r], R.zs[n]);
+                R.zs[n] = fmaf(p1, vz[x][r + 1], R.zs[n]);
+                pk[2 * x + (r >> 1)] = pack_f16(p0 * vs[x][r], p1 * vs[x][r + 1]);
+            }
+        w[n] = __builtin_bit_cast(f16x8, pk);
+    }
+    unsigned lo[4], hi[4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            lo[2 * x + r] = lo_halves(c.v[x][2 * r], c.v[x][2 * r + 1]);
+            hi[2 * x + r] = hi_halves(c.v[x][2 * r], c.v[x][2 * r + 1]);
+        }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        u32x4 a;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) a[r] = ((j < 4 ? lo[r] : hi[r]) >> (4 * (j & 3))) & 0x000F000Fu;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) R.o[n][j] = mma(__builtin_bit_cast(f16x8, a), w[n], R.o[n][j]);
+    }
+}
+
+__device__ __forceinline__ bool any_not_finite(unsigned w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// 32 suffix tokens from j0 on; k, v point at the trace's first token and the head, rows are `stride` elements apart; a row
+// sees tokens up to its own (tok).  Products in bfloat16, probabilities in two terms.
+template <int NQ>
+__device__ __forceinline__ void suffix_chunk(Rows4<NQ> &R, const bf16 *k, const bf16 *v, size_t stride, int j0, int S, const int (&tok)[NQ],
+                                             int n15, int g) {
+    f32x4 sc[NQ][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const bf16 *row = k + (size_t)min(j0 + 16 * x + n15, S - 1) * stride + 8 * g;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bf16x8 a = *(const bf16x8 *)(row + 32 * i);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) sc[n][x] = mma(a, R.q[n][i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[n][x]);
+        }
+    }
+    u32x4 vw[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        const int j = j0 + 16 * (t >> 2) + 4 * g + (t & 3);
+        vw[t] = *(const u32x4 *)(v + (size_t)min(j, S - 1) * stride + 8 * n15);
+        if (j >= S) vw[t] = u32x4{0u, 0u, 0u, 0u};
+    }
+    float t_max[NQ];
+    bool masked = false;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        t_max[n] = -INFINITY;
+        masked |= j0 + 31 > tok[n];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float s = j0 + 16 * x + 4 * g + r <= tok[n] ? sc[n][x][r] * SCALE_LOG2 : -INFINITY;
+                sc[n][x][r] = s;
+                t_max[n] = fmaxf(t_max[n], s + 127.f);
+            }
+    }
+    raise<NQ>(R, t_max);
+    u32x4 hi[NQ], lo[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const float ref = R.m[n] - 132.f;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {
+                float p0 = __builtin_amdgcn_exp2f(sc[n][x][r] - ref), p1 = __builtin_amdgcn_exp2f(sc[n][x][r + 1] - ref);
+                R.l[n] += p0;
+                R.l[n] += p1;
+                p0 *= V_UNIT;
+                p1 *= V_UNIT;
+                sc[n][x][r] = p0;
+                sc[n][x][r + 1] = p1;
+                const unsigned h = pack_bf16(p0, p1);
+                hi[n][2 * x + (r >> 1)] = h;
+                lo[n][2 * x + (r >> 1)] = pack_bf16(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+            }
+    }
+    // A value that is not a finite number may only reach the rows that see its token, but the matrix product takes 0 times
+    // it into every row: such values are taken out and added one by one where they are seen.
+    if (__any(masked)) {
+        bool bad = false;
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad |= any_not_finite(vw[t][e]);
+        if (__any(bad)) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if ((vw[t][e] & 0x7f80u) == 0x7f80u) vw[t][e] &= 0xffff0000u;
+                    if ((vw[t][e] & 0x7f800000u) == 0x7f800000u) vw[t][e] &= 0xffffu;
+                }
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    for (int g2 = 0; g2 < 4; ++g2) {
+                        const int j = j0 + 16 * x + 4 * g2 + r;
+                        if (j >= S) continue;
+                        const unsigned short *row = (const unsigned short *)(v + (size_t)j * stride + 32 * g);
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) {
+                            const float p = __shfl(sc[n][x][r], n15 + 16 * g2, 64);
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                const unsigned bits = row[c];
+                                if ((bits & 0x7f80u) == 0x7f80u && j <= tok[n]) R.o[n][c & 7][c >> 3] += p * __uint_as_float(bits << 16);
+                            }
+                        }
+                    }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        u32x4 a;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            a[r] = j & 1 ? hi_halves(vw[2 * r][j >> 1], vw[2 * r + 1][j >> 1]) : lo_halves(vw[2 * r][j >> 1], vw[2 * r + 1][j >> 1]);
+        const bf16x8 av = __builtin_bit_cast(bf16x8, a);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, hi[n]), R.o[n][j]);
+            R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, lo[n]), R.o[n][j]);
+        }
+    }
+}
+
+// Trace of an item (entries of `start` behind the last trace are n_items).
+__device__ __forceinline__ int plan_trace(const uint32_t *start, unsigned item, int lane) {
+    int b = 0;
+#pragma unroll
+    for (int k = 0; k < ATT_TRACES / 64; ++k) b += __popcll(__ballot(start[1 + lane + 64 * k] <= item));
+    return __builtin_amdgcn_readfirstlane(min(b, ATT_TRACES - 1));
+}
+
+constexpr int O_PAD = 132;            // floats from row to row of O in LDS
+
+// WR x WK wavefronts: WR take different rows, WK different chunks of keys.
+template <int NQ, int WR, int WK>
+__global__ __launch_bounds__(WR * WK * 64, NQ == 1 ? 3 : 2) void kv4_attn_kernel(Kv4Attn a, AttnPlan4 plan, float *part_o, float2 *part_ml) {
+    constexpr int ROWS = 16 * NQ * WR;
+    __shared__ float s_o[WK > 1 ? WK * ROWS * O_PAD : 1];
+    __shared__ float2 s_ml[WK > 1 ? WK * ROWS : 1];
+    const Kv4Batch &kv = a.b;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+    const int n15 = lane & 15, g = lane >> 4;
+    unsigned item = blockIdx.x;
+    if (plan.swizzle) {               // workgroups are dealt out over 8 L2 caches: neighbours in the list, which share keys, to one
+        const unsigned per = gridDim.x / 8, x = item % 8, rest = gridDim.x % 8;
+        item = x * per + min(x, rest) + item / 8;
+    }
+    const int bi = plan_trace(plan.start, item, lane), trace = min(plan.b0 + bi, kv.B - 1);
+    const int G = a.Hq / kv.Hkv;
+    const int t0 = min(max(kv.cu[trace], 0), kv.T - 1), S = min(max(kv.cu[trace + 1] - t0, 1), kv.T - t0);
+    const int L = min(max(kv.plens[trace], 0), kv.max_blocks * 16);
+    const int n_rows = G * S, n_tiles = (n_rows + ROWS - 1) / ROWS, P = plan.pieces[bi];
+    const int local = (int)(item - plan.start[bi]);
+    const int rt = local % n_tiles, piece = local / n_tiles % P, h = local / n_tiles / P;
+    if (h >= kv.Hkv) return;          // (only where device and host lengths differ)
+    const int row0 = rt * ROWS + wr * 16 * NQ;
+
+    Rows4<NQ> R;
+    int tok[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int row = min(row0 + 16 * n + n15, n_rows - 1);
+        tok[n] = row / G;
+        const bf16 *q = a.q + ((size_t)(t0 + tok[n]) * a.Hq + h * G + row % G) * 128 + 8 * g;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            R.q[n][i] = *(const bf16x8 *)(q + 32 * i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += (float)R.q[n][i][e];
+        }
+        R.q_sum[n] = sum_over_g(sum);
+        R.q_off[n] = f32x4{1.f, 1.f, 1.f, 1.f} * (-24.f * R.q_sum[n]);
+        R.m[n] = M_NONE;
+        R.l[n] = R.zs[n] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) R.o[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // chunks of this piece: cached ones first, then the suffix as far as the tile's last row sees it
+    const int n_cached = (L + 31) >> 5, tok_hi = (min((rt + 1) * ROWS, n_rows) - 1) / G, n_all = n_cached + (tok_hi >> 5) + 1;
+    const int c_begin = (int)((int64_t)n_all * piece / P), c_end = (int)((int64_t)n_all * (piece + 1) / P);
+    int c = c_begin + wk;
+    const int c_stop = min(c_end, n_cached);
+    if (c < c_stop) {
+        const int32_t *table = kv.table + (size_t)trace * kv.max_blocks;
+        const uint8_t *head = kv.pages + (size_t)h * KV4_PAGE;
+        const size_t block_bytes = (size_t)kv.Hkv * KV4_PAGE;
+        const unsigned at16 = lane * 16, at_g = g * 16;
+        int ids = 0, left = 0;        // block numbers of the next 32 chunks, two lanes each
+        auto load = [&](Chunk4 &d, int cc) {
+            if (left == 0) {
+                const int page = 2 * (cc + WK * (lane >> 1)) + (lane & 1);
+                ids = min(max(table[min(page, kv.max_blocks - 1)], 0), kv.n_blocks - 1);
+                left = 32;
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint8_t *page = head + (size_t)__builtin_amdgcn_readlane(ids, 2 * (32 - left) + x) * block_bytes;
+                d.k[x] = *(const u32x4 *)(page + at16);
+                d.v[x] = *(const u32x4 *)(page + KV4_V + at16);
+                d.kp[x] = *(const u32x4 *)(page + KV4_KP + at_g);
+                d.vp[x] = *(const u32x4 *)(page + KV4_VP + at_g);
+            }
+            --left;
+        };
+        Chunk4 c0, c1;
+        load(c0, c);
+        for (;;) {
+            if (c + WK < c_stop) load(c1, c + WK);
+            cached_chunk<NQ>(R, c0, L - 32 * c, g);
+            c += WK;
+            if (c >= c_stop) break;
+            if (c + WK < c_stop) load(c0, c + WK);
+            cached_chunk<NQ>(R, c1, L - 32 * c, g);
+            c += WK;
+            if (c >= c_stop) break;
+        }
+    }
+    if (c_end > n_cached) {
+        const size_t stride = (size_t)kv.Hkv * 128;
+        const bf16 *k = a.k + (size_t)t0 * stride + (size_t)h * 128, *v = a.v + (size_t)t0 * stride + (size_t)h * 128;
+        const int my_hi = (min(row0 + 16 * NQ, n_rows) - 1) / G;      // (negative rows cannot be: row0 may lie behind the last row)
+        for (; c < c_end; c += WK)
+            if (32 * (c - n_cached) <= my_hi) suffix_chunk<NQ>(R, k, v, stride, 32 * (c - n_cached), S, tok, n15, g);
+    }
+
+    const bool direct = P == 1;
+    const size_t rec = (size_t)plan.part[bi] + ((size_t)(h * n_tiles + rt) * P + piece);
+    auto store8 = [&](int row_in_tile, int col, const float (&o)[8], float m, float l, bool first) {
+        const int row = rt * ROWS + row_in_tile;
+        if (row >= n_rows) return;
+        if (direct) {
+            const float f = 1.f / l;
+            const u32x4 r = {pack_bf16(o[0] * f, o[1] * f), pack_bf16(o[2] * f, o[3] * f), pack_bf16(o[4] * f, o[5] * f), pack_bf16(o[6] * f, o[7] * f)};
+            *(u32x4 *)(a.out + ((size_t)(t0 + row / G) * a.Hq + h * G + row % G) * 128 + col) = r;
+        } else {
+            float *dst = part_o + (rec * ROWS + row_in_tile) * 128 + col;
+            *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
+            *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
+            if (first) part_ml[rec * ROWS + row_in_tile] = make_float2(m, l);
+        }
+    };
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const float l = sum_over_g(R.l[n]), zs = sum_over_g(R.zs[n]);
+        const int row = wr * 16 * NQ + 16 * n + n15;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = fmaf(R.o[n][j][r], 1.f / V_UNIT, zs);
+            if constexpr (WK == 1) {
+                store8(row, 32 * g + 8 * r, o, R.m[n], l, g == 0 && r == 0);
+            } else {
+                float *dst = s_o + (wk * ROWS + row) * O_PAD + 32 * g + 8 * r;
+                *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
+                *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
+                if (g == 0 && r == 0) s_ml[wk * ROWS + row] = make_float2(R.m[n], l);
+            }
+        }
+    }
+    if constexpr (WK > 1) {
+        __syncthreads();
+        for (int at = tid; at < ROWS * 16; at += WR * WK * 64) {
+            const int row = at >> 4, col = (at & 15) * 8;
+            float m = M_NONE;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) m = fmaxf(m, s_ml[w * ROWS + row].x);
+            float l = 0.f, o[8] = {};
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const float2 ml = s_ml[w * ROWS + row];
+                const float f = __builtin_amdgcn_exp2f(ml.x - m);
+                l += f * ml.y;
+                const float *src = s_o + (w * ROWS + row) * O_PAD + col;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] += f * src[e];
+            }
+            store8(row, col, o, m, l, col == 0);
+        }
+    }
+}
+
+// One wavefront per (head, row) of the traces that were cut: a lane has two columns.
+__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 plan, int tile_rows, const float *__restrict__ part_o,
+                                                        const float2 *__restrict__ part_ml) {
+    const Kv4Batch &kv = a.b;
+    const int lane = threadIdx.x & 63;
+    const unsigned at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (at >= (unsigned)plan.n_merge_rows) return;
+    const int bi = plan_trace(plan.mrow, at, lane), trace = min(plan.b0 + bi, kv.B - 1), G = a.Hq / kv.Hkv, P = plan.pieces[bi];
+    const int t0 = min(max(kv.cu[trace], 0), kv.T - 1), S = min(max(kv.cu[trace + 1] - t0, 1), kv.T - t0);
+    const int n_rows = G * S, n_tiles = (n_rows + tile_rows - 1) / tile_rows, local = (int)(at - plan.mrow[bi]), h = local / n_rows, row = local % n_rows;
+    if (h >= kv.Hkv) return;
+    const size_t rec = (size_t)plan.part[bi] + (size_t)(h * n_tiles + row / tile_rows) * P;
+    const size_t first = rec * tile_rows + row % tile_rows;
+    float m = M_NONE;
+    for (int p = 0; p < P; ++p) m = fmaxf(m, part_ml[first + (size_t)p * tile_rows].x);
+    float l = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int p = 0; p < P; ++p) {
+        const float2 ml = part_ml[first + (size_t)p * tile_rows], o = *(const float2 *)(part_o + (first + (size_t)p * tile_rows) * 128 + 2 * lane);
+        const float f = __builtin_amdgcn_exp2f(ml.x - m);
+        l += f * ml.y;
+        o0 += f * o.x;
+        o1 += f * o.y;
+    }
+    *(unsigned *)(a.out + ((size_t)(t0 + row / G) * a.Hq + h * G + row % G) * 128 + 2 * lane) = pack_bf16(o0 / l, o1 / l);
+}
+
+// The launches of a batch: up to ATT_TRACES traces each.
+struct Launch4 {
+    AttnPlan4 plan;
+    int nq, wr, wk;
+    size_t records;                   // partial records of tile_rows rows
+    int tile_rows() const { return 16 * nq * wr; }
+};
+constexpr int ATT_SLOTS = 1024;       // items a launch is cut into at least, as far as ATT_MIN_CHUNKS lets it
+constexpr int ATT_MIN_CHUNKS = 32;
+
+void plan_launch(Launch4 &p, const int32_t *h_cu, const int32_t *h_lens, int b0, int nb, int Hq, int Hkv) {
+    const int G = Hq / Hkv;
+    int64_t max_rows = 0;
+    for (int b = b0; b < b0 + nb; ++b) max_rows = std::max<int64_t>(max_rows, (int64_t)G * (h_cu[b + 1] - h_cu[b]));
+    if (max_rows <= 16) { p.nq = 1; p.wr = 1; p.wk = 4; }
+    else if (max_rows <= 64) { p.nq = 2; p.wr = 1; p.wk = 4; }
+    else { p.nq = 2; p.wr = 4; p.wk = 1; }
+    const int rows = p.tile_rows();
+    auto tiles = [&](int b) { return ((int64_t)G * (h_cu[b + 1] - h_cu[b]) + rows - 1) / rows; };
+    auto chunks = [&](int b) { return ((int64_t)h_lens[b] + 31) / 32 + ((int64_t)h_cu[b + 1] - h_cu[b] + 31) / 32; };
+    int64_t total = 0;
+    for (int b = b0; b < b0 + nb; ++b) total += Hkv * tiles(b) * chunks(b);
+    const int64_t per = std::max<int64_t>(ATT_MIN_CHUNKS, (total + ATT_SLOTS - 1) / ATT_SLOTS);
+    p.plan.b0 = b0;
+    p.records = 0;
+    int64_t items = 0, mrows = 0;
+    bool many_tiles = false;
+    for (int i = 0; i < ATT_TRACES; ++i) {
+        p.plan.start[i] = (uint32_t)items;
+        p.plan.mrow[i] = (uint32_t)mrows;
+        p.plan.part[i] = (uint32_t)p.records;
+        p.plan.pieces[i] = 1;
+        if (i >= nb) continue;
+        const int b = b0 + i;
+        const int64_t P = std::min<int64_t>((chunks(b) + per - 1) / per, 1024), n = Hkv * tiles(b) * P;
+        p.plan.pieces[i] = (uint16_t)P;
+        many_tiles |= tiles(b) > 1;
+        items += n;
+        if (P > 1) {
+            p.records += n;
+            mrows += (int64_t)Hkv * G * (h_cu[b + 1] - h_cu[b]);
+        }
+    }
+    p.plan.start[ATT_TRACES] = (uint32_t)items;
+    p.plan.mrow[ATT_TRACES] = (uint32_t)mrows;
+    p.plan.n_items = (int32_t)items;
+    p.plan.n_merge_rows = (int32_t)mrows;
+    p.plan.swizzle = many_tiles;
 }
 
 }  // namespace
@@ -205,11 +658,38 @@ hipError_t launch_kv4_read(const Kv4Batch &b, float *k, float *v, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t kv4_attn_scratch(const int32_t *, const int32_t *, int, int, int) { return 0; }
+namespace {
+size_t part_o_bytes(const Launch4 &p) { return p.records * p.tile_rows() * 128 * sizeof(float); }
+size_t part_ml_bytes(const Launch4 &p) { return p.records * p.tile_rows() * sizeof(float2); }
+}  // namespace
 
-hipError_t launch_kv4_attn(const Kv4Attn &a, const int32_t *, const int32_t *, void *, hipStream_t s) {
-    kv4_attn_kernel<<<a.b.T * a.Hq, 64, 0, s>>>(a);
-    return hipGetLastError();
+size_t kv4_attn_scratch(const int32_t *h_cu, const int32_t *h_lens, int B, int Hq, int Hkv) {
+    size_t need = 0;
+    Launch4 p;
+    for (int b0 = 0; b0 < B; b0 += ATT_TRACES) {      // (the launches follow one another: each may use all of it)
+        plan_launch(p, h_cu, h_lens, b0, std::min(ATT_TRACES, B - b0), Hq, Hkv);
+        need = std::max(need, part_o_bytes(p) + part_ml_bytes(p));
+    }
+    return need;
+}
+
+hipError_t launch_kv4_attn(const Kv4Attn &a, const int32_t *h_cu, const int32_t *h_lens, void *scratch, hipStream_t s) {
+    Launch4 p;
+    for (int b0 = 0; b0 < a.b.B; b0 += ATT_TRACES) {
+        plan_launch(p, h_cu, h_lens, b0, std::min(ATT_TRACES, a.b.B - b0), a.Hq, a.b.Hkv);
+        float *part_o = (float *)scratch;
+        float2 *part_ml = (float2 *)((char *)scratch + part_o_bytes(p));
+        const int threads = 64 * p.wr * p.wk;
+        if (p.nq == 1) kv4_attn_kernel<1, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else if (p.wr == 1) kv4_attn_kernel<2, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else kv4_attn_kernel<2, 4, 1><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (p.plan.n_merge_rows) {
+            kv4_merge_kernel<<<(p.plan.n_merge_rows + 3) / 4, 256, 0, s>>>(a, p.plan, p.tile_rows(), part_o, part_ml);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+    }
+    return hipSuccess;
 }
 
 }  // namespace cs

@@ -10,8 +10,8 @@ HD, PAGE = 128, 2176
 def quantise(x):
     """Rows [..., 128] -> codes (int64), s, z (halves), as the header defines them."""
     x = x.double().clamp(-65504.0, 65504.0)
-    z = x.min(-1).values.float().half() + 0.0          # (which of two zeros min returns is open: z is never -0)
-    s = ((x.max(-1).values - z.double()) / 15.0).float().half()
+    z = x.min(-1).values.float().half() + 0.0          # (which of two zeros min and max return is open: never -0)
+    s = ((x.max(-1).values - z.double()) / 15.0).float().half() + 0.0
     sd = s.double()[..., None]
     c = torch.round((x - z.double()[..., None]) / torch.where(sd > 0, sd, torch.ones_like(sd)))      # ties to even
     c = torch.where(sd > 0, c, torch.zeros_like(c)).clamp(0, 15).to(torch.int64)
@@ -82,12 +82,13 @@ def attention(pages, table, q, k, v, cu, lens, Hq, Hkv):
     header's numerics allow, element by element.
 
     Terms of the bound, beside half a bf16 step of the result (2^-8 |o|):
-      - probabilities times s are halves: half a step, 2^-11, of p_j s_j (|c_j - 8|); suffix probabilities have two bf16
+      - probabilities times s are halves: half a step, 2^-11, of p_j s_j c_j; suffix probabilities have two bf16
         terms, 2^-16;
       - scores are fp32: q (16 + c) sums over 128 products exact each, so an error of 136 2^-24 sum |q| (16 + 15 + 24) s
         and two roundings of s acc + z' sum q, which moves a probability by that times log(e) = the same relative to it;
         twice, for numerator and denominator; exp2 and the shift cost 2^-20 of p (scores up to 2^6) more;
-      - sums over n keys: added in steps of 32, wavefronts and pieces apart: (n / 32 + 64) 2^-24 of the absolute sum."""
+      - sums over n keys: added in steps of 32, wavefronts and pieces apart: (n / 32 + 64) 2^-24 of the absolute sum,
+        in which s c and z count apart."""
     T, G = q.shape[0], Hq // Hkv
     out = torch.empty(T, Hq * HD, dtype=torch.float64, device=q.device)
     tol = torch.empty_like(out)
@@ -103,7 +104,7 @@ def attention(pages, table, q, k, v, cu, lens, Hq, Hkv):
                 V = vz[:, None] + vs[:, None] * vc.reshape(-1, HD)[:L]
             else:
                 K = V = torch.empty(0, HD, dtype=torch.float64, device=q.device)
-                ks = kz = vs = torch.empty(0, dtype=torch.float64, device=q.device)
+                ks = kz = torch.empty(0, dtype=torch.float64, device=q.device)
             Ks, Vs = k[t0:t0 + S, h].double(), v[t0:t0 + S, h].double()
             Q = q[t0:t0 + S, h * G:(h + 1) * G].double().reshape(S * G, HD)
             s = Q @ torch.cat((K, Ks)).t() / math.sqrt(HD)
@@ -115,11 +116,12 @@ def attention(pages, table, q, k, v, cu, lens, Hq, Hkv):
             qa = Q.abs().sum(-1, keepdim=True)
             es = 2.0 ** -24 * qa * torch.cat((138 * (55 * ks + 2 * kz.abs()), 138 * Ks.abs().max(-1).values)) / math.sqrt(HD)
             es = torch.where(p > 0, es, torch.zeros_like(es))
-            reach = torch.cat((V.abs() + 8 * vs[:, None], Vs.abs()))
+            reach = torch.cat((V.abs(), Vs.abs()))
+            apart = torch.cat((vz.abs()[:, None] + (V - vz[:, None]).abs(), Vs.abs())) if L else reach
             spread = (p * es) @ reach + (p * es).sum(-1, keepdim=True) * (p @ reach)
             rel = torch.cat((torch.full((L,), 2.0 ** -11, dtype=torch.float64, device=q.device), torch.full((S,), 2.0 ** -16, dtype=torch.float64, device=q.device)))
             sums = ((L + S) / 32 + 64) * 2.0 ** -24 * 6 + 2.0 ** -19
-            w = 2.0 ** -8 * o.abs() + 1.01 * spread + (p * rel) @ torch.cat((8 * vs[:, None].expand(-1, HD), Vs.abs())) + sums * (p @ reach)
+            w = 2.0 ** -8 * o.abs() + 1.01 * spread + (p * rel) @ torch.cat(((V - vz[:, None]).abs() if L else V, Vs.abs())) + sums * (p @ apart)
             out[t0:t0 + S, h * G * HD:(h + 1) * G * HD] = o.view(S, G * HD)
             tol[t0:t0 + S, h * G * HD:(h + 1) * G * HD] = w.view(S, G * HD)
     return out, tol
