@@ -137,7 +137,7 @@ def _load() -> C.CDLL:
     lib.confspec_op_workspace_slices.restype = C.c_int
     lib.confspec_op_workspace_slices.argtypes = [vp, i32, i32, P(Batch), P(sz), P(sz), P(i32), P(sz)]
     lib.confspec_op_kv4_append.restype = C.c_int
-    lib.confspec_op_kv4_append.argtypes = [vp, P(KV4), P(Batch), i32, vp, C.c_int64, vp, P(i32), vp, vp, vp, vp]
+    lib.confspec_op_kv4_append.argtypes = [vp, P(KV4), P(Batch), i32, vp, C.c_int64, vp, vp, vp, vp, vp, vp]
     lib.confspec_op_kv4_read.restype = C.c_int
     lib.confspec_op_kv4_read.argtypes = [vp, P(KV4), P(Batch), i32, vp, vp, vp]
     lib.confspec_op_kv4_attention.restype = C.c_int
@@ -182,10 +182,29 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _current_stream_getter():
+    """The handle of torch's current stream, without a Stream object where this torch offers it (0.2 us instead of 2.8)."""
+    import torch
+    raw, dev = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or dev is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+
+    def get():
+        if not torch.cuda.is_initialized():
+            torch.cuda.init()
+        return raw(dev())
+    return get
+
+
+_current_stream = None
+
+
 def _stream_handle(stream) -> Optional[int]:
+    global _current_stream
     if stream is None:
-        import torch
-        stream = torch.cuda.current_stream()
+        if _current_stream is None:
+            _current_stream = _current_stream_getter()
+        return _current_stream() or None
     h = getattr(stream, "cuda_stream", stream)
     return h if h else None
 
@@ -373,9 +392,9 @@ def confspec_op_kv4_append(ctx, kv: KV4, batch: Batch, layer: int, qkv, n_append
     host int32 array, or both None (every token)."""
     import numpy as np
     hn = None if h_n_append is None else np.ascontiguousarray(h_n_append, dtype=np.int32)
-    hp = None if hn is None else hn.ctypes.data_as(C.POINTER(C.c_int32))
     _check(ctx, lib.confspec_op_kv4_append(ctx, C.byref(kv), C.byref(batch), layer, _ptr(qkv),
-                                           qkv.stride(0) if qkv_stride is None else qkv_stride, _ptr(n_append), hp, _ptr(q),
+                                           qkv.stride(0) if qkv_stride is None else qkv_stride, _ptr(n_append),
+                                           None if hn is None else hn.ctypes.data, _ptr(q),
                                            _ptr(k), _ptr(v), _stream_handle(stream)))
 
 

@@ -355,7 +355,7 @@ hipError_t launch_kv4_attn(const Kv4Attn &a, const int32_t *h_cu, const int32_t 
 
 // ---- products with 4-bit weights (w4.hip) ----
 // Records of 16 rows x 128 k: [N / 16][ceil(K / 128)] of the key codes' layout (row for token) and 128 / group x 16 pairs (s, z).
-constexpr int W4_MAX_ROWS = 128;
+constexpr int W4_MAX_ROWS = 128, W4_MAX_K = 1 << 22;      // 32-bit offsets into A
 __host__ __device__ inline int w4_record(int group) { return 1024 + 64 * (128 / group); }
 __host__ __device__ inline int w4_kblocks(int K) { return (K + 127) / 128; }
 hipError_t launch_w4_pack(const uint8_t *codes, const __half *scales, const __half *zeros, uint8_t *dst, int N, int K, int group,

@@ -1,19 +1,21 @@
 // Products of up to 128 rows with 4-bit weights.  Record format: confspec_int4.h, kernels.h.
 #include "kernels.h"
+#include <algorithm>
+#include <cstdlib>
 
 namespace cs {
 
 namespace {
 
-// Row of the matrix that is row m of the 16 of tile nt.  A gate/up matrix has gate f, f + 1 and up f, f + 1 in turn, so
-// that the four rows a lane gets from a matrix instruction are two finished pairs.
+// Row of the matrix that is row m of the 16 of tile nt.  A gate/up matrix has eight gate rows and their eight up rows in a
+// tile, so that a lane finds the other half of its pair eight lanes away.
 __device__ __forceinline__ int w4_source_row(int nt, int m, int N, int gate_up) {
     if (!gate_up) return nt * 16 + m;
-    const int f = nt * 8 + (m >> 2) * 2 + (m & 1);
-    return (m & 2) ? N / 2 + f : f;
+    const int f = nt * 8 + (m & 7);
+    return (m & 8) ? N / 2 + f : f;
 }
 
-// One workgroup per record: 256 words, then the pairs (s, z).  What lies behind K is zero.
+// One workgroup per record: 256 words, then the pairs (s, z / 16) of row 0's groups, row 1's, ...  What lies behind K is zero.
 __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t *__restrict__ codes, const __half *__restrict__ scales,
                                                       const __half *__restrict__ zeros, uint8_t *__restrict__ dst, int N, int K,
                                                       int group, int gate_up, int record, int n_kb) {
@@ -31,49 +33,206 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t *__restrict_
     }
     const int ng = 128 / group;
     if (tid < ng * 16) {
-        const int g = kb * ng + tid / 16, m = tid & 15;
+        const int m = tid / ng, g = kb * ng + tid % ng;
         unsigned p = 0;
         if (g < K / group) {
             const size_t at = (size_t)w4_source_row(nt, m, N, gate_up) * (K / group) + g;
-            p = (unsigned)__half_as_ushort(scales[at]) | (unsigned)__half_as_ushort(zeros ? zeros[at] : __float2half_rn(8.f)) << 16;
+            const float z = zeros ? __half2float(zeros[at]) : 8.f;
+            p = (unsigned)__half_as_ushort(scales[at]) | (unsigned)__half_as_ushort(__float2half_rn(z * 0.0625f)) << 16;
         }
         ((unsigned *)(rec + 1024))[tid] = p;
     }
 }
 
-__device__ float w4_dot(const W4Gemm &a, int m, int n_tile, int row) {
-    const int n_kb = w4_kblocks(a.K), record = w4_record(a.group);
-    float acc = 0.f;
-    for (int k0 = 0; k0 < a.K; k0 += a.group) {
-        const uint8_t *rec = a.W + ((size_t)n_tile * n_kb + (k0 >> 7)) * record;
-        const unsigned p = ((const unsigned *)(rec + 1024))[((k0 & 127) / a.group) * 16 + row];
-        const float s = __half2float(__ushort_as_half((unsigned short)(p & 0xffff))), z = __half2float(__ushort_as_half((unsigned short)(p >> 16)));
-        float part = 0.f;
-        for (int k = k0; k < k0 + a.group; k += 8) {
-            const unsigned w = ((const unsigned *)rec)[(((k & 31) >> 3) * 16 + row) * 4 + ((k & 127) >> 5)];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                part += __bfloat162float(a.A[(size_t)m * a.K + k + e]) * ((float)((w >> (4 * ((e >> 1) + 4 * (e & 1)))) & 15) - z);
-        }
-        acc += s * part;
-    }
-    return acc;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// Eight codes as bfloat16 16 + c: element 2 k and 2 k + 1 are nibbles k and k + 4.
+struct CodeBits { unsigned mask, one; };   // in registers: one and-or takes both only if neither is a literal
+__device__ __forceinline__ CodeBits code_bits() {
+    CodeBits b;
+    asm("s_mov_b32 %0, 0x780078" : "=s"(b.mask));
+    asm("v_mov_b32 %0, 0x41804180" : "=v"(b.one));
+    return b;
+}
+__device__ __forceinline__ bf16x8 code_operand(unsigned w, CodeBits b) {
+    const unsigned M = b.mask, C = b.one;
+    const u32x4 r = {((w << 3) & M) | C, ((w >> 1) & M) | C, ((w >> 5) & M) | C, ((w >> 9) & M) | C};
+    return __builtin_bit_cast(bf16x8, r);
 }
 
-// A thread per output.
-__global__ __launch_bounds__(256) void w4_gemm_kernel(W4Gemm a) {
-    const int n_out = a.epi == EPI_SWIGLU ? a.N / 2 : a.N;
-    const long at = (long)blockIdx.x * 256 + threadIdx.x;
-    if (at >= (long)a.M * n_out) return;
-    const int m = (int)(at / n_out), n = (int)(at % n_out);
-    if (a.epi == EPI_SWIGLU) {
-        const int f = n & 7, row = (f >> 1) * 4 + (f & 1);
-        const float g = w4_dot(a, m, n >> 3, row), u = w4_dot(a, m, n >> 3, row + 2);
-        ((bf16 *)a.out)[at] = __float2bfloat16(g / (1.f + expf(-g)) * u);
-    } else {
-        const float y = w4_dot(a, m, n >> 4, n & 15);
-        ((float *)a.out)[at] = a.epi == EPI_RESID_F32 ? a.resid[at] + y : y;
+// A wavefront has 16 MT rows of A, 16 NT rows of W and every W-th block of 128 k; the wavefronts of a workgroup have the same
+// rows and add up in LDS, in a fixed order.
+//  * A record's codes are the second operand of four 16x16x32 products as they lie in memory, 16 bytes a lane, a code c as
+//    the bfloat16 16 + c (its four bits put into the mantissa of 16), which is exact.  Before them goes a product with
+//    -16 everywhere: it takes the offset out, and leaves -16 sum(a) of the group, which z / 16 is multiplied by.
+//  * A lane has one row of W and four rows of A in the result, so that a group costs two multiply-adds a result, which take s and z
+//    as the halves they are: sum += s (part - z sum(a)).
+// Bound by the bytes of W while rows are few; every workgroup reads its rows of A from L2.
+template <int NG>
+struct Params;
+template <> struct Params<1> { typedef unsigned T; static __device__ unsigned get(T p, int) { return p; } };
+template <> struct Params<2> { typedef uint2 T; static __device__ unsigned get(T p, int g) { return g ? p.y : p.x; } };
+template <> struct Params<4> { typedef u32x4 T; static __device__ unsigned get(T p, int g) { return p[g]; } };
+
+constexpr int max_waves(int MT, int) { return MT == 1 ? 16 : 8; }   // of a workgroup: what the registers of a wavefront leave room for
+
+// Loads of 16, 8 or 4 bytes from a wave-uniform base plus a byte offset per lane; offsets at or past the end read zeros, and
+// touch no memory: so blocks behind the last one need no case of their own.
+struct Loads {
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ Loads(const void *base, unsigned bytes) : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000)) {}
+    __device__ void get(unsigned off, u32x4 &v) const { v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)off, 0, 0)); }
+    __device__ void get(unsigned off, uint2 &v) const { v = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, (int)off, 0, 0)); }
+    __device__ void get(unsigned off, unsigned &v) const { v = __builtin_amdgcn_raw_buffer_load_b32(rsrc, (int)off, 0, 0); }
+};
+constexpr unsigned PAST_END = 0x80000000u;
+
+// AL: loads of four rows of A each a block takes, at least as many as there are rows.
+template <int AL, int NT, int NG>
+struct Block {                        // operands of one block of k as they come from memory
+    u32x4 a[AL], w[NT];
+    typename Params<NG>::T p[NT];
+};
+
+template <int MT, int AL, int NT, int NG, int D>
+__global__ __launch_bounds__(64 * max_waves(MT, NT)) void w4_gemm_kernel(W4Gemm g, int n_mb, int W) {
+    extern __shared__ u32x4 s_mem[];
+    constexpr int REC = 1024 + 64 * NG;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n15 = lane & 15, kg = lane >> 4;
+    const int mb = blockIdx.x % n_mb, nb = blockIdx.x / n_mb, m0 = mb * 16 * MT, t0 = nb * NT, n_tiles = g.N >> 4, n_kb = w4_kblocks(g.K);
+    const unsigned w_at = lane * 16, p_at = 1024 + n15 * 4 * NG, tile_bytes = (unsigned)n_kb * REC;
+    const Loads A(g.A, (unsigned)g.M * (unsigned)g.K * 2u), Wt(g.W + (size_t)t0 * tile_bytes, (unsigned)min(NT, n_tiles - t0) * tile_bytes);
+    unsigned a_at[AL];                // byte offsets of the lane's rows of A (W4_MAX_K keeps the matrix below 2^31 bytes)
+#pragma unroll
+    for (int j = 0; j < AL; ++j) a_at[j] = (unsigned)min(m0 + 4 * j + kg, g.M - 1) * (unsigned)g.K * 2u;
+    u32x4 *const s_a = s_mem + wave * MT * 256;
+    f32x4 sum[MT][NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sum[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const CodeBits bits = code_bits();
+    const u32x4 neg16_bits = {0xC180C180u, 0xC180C180u, 0xC180C180u, 0xC180C180u};
+    const bf16x8 neg16 = __builtin_bit_cast(bf16x8, neg16_bits);
+
+    auto load = [&](Block<AL, NT, NG> &b, int kb) {
+        const unsigned k = (unsigned)kb * 256u + 16u * n15, at = (int)k < 2 * g.K ? k : PAST_END;      // (K a multiple of 32: 64 bytes)
+#pragma unroll
+        for (int j = 0; j < AL; ++j) A.get(a_at[j] + at, b.a[j]);
+        const unsigned rec = kb < n_kb ? (unsigned)kb * REC : PAST_END;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            Wt.get(rec + t * tile_bytes + w_at, b.w[t]);
+            Wt.get(rec + t * tile_bytes + p_at, b.p[t]);
+        }
+        __builtin_amdgcn_sched_barrier(0);       // (loads stay ahead of the products before them in time)
+    };
+    // Rows of A: 16 lanes have 256 consecutive bytes of a row, the operand wants a row a lane; through LDS, where row r keeps
+    // its 16-byte piece v at v ^ r % 16: 16 lanes then meet all banks both ways.
+    auto compute = [&](const Block<AL, NT, NG> &b) {
+#pragma unroll
+        for (int j = 0; j < AL; ++j) s_a[(4 * j + kg) * 16 + (n15 ^ ((4 * j + kg) & 15))] = b.a[j];
+        __builtin_amdgcn_wave_barrier();
+        bf16x8 a[MT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[m][i] = __builtin_bit_cast(bf16x8, s_a[(16 * m + n15) * 16 + ((4 * i + kg) ^ n15)]);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < NG; ++q) {
+            f32x4 off[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                off[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 4 / NG; ++i) off[m] = mma(a[m][q * (4 / NG) + i], neg16, off[m]);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                f32x4 part[MT];
+#pragma unroll
+                for (int i = 0; i < 4 / NG; ++i) {
+                    const bf16x8 c = code_operand(b.w[t][q * (4 / NG) + i], bits);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) part[m] = mma(a[m][q * (4 / NG) + i], c, i == 0 ? off[m] : part[m]);
+                }
+                const f16x2 sz = __builtin_bit_cast(f16x2, Params<NG>::get(b.p[t], q));
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum[m][t][r] = fmaf((float)sz[0], fmaf((float)sz[1], off[m][r], part[m][r]), sum[m][t][r]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    {
+        Block<AL, NT, NG> b[D];       // D - 1 blocks on their way while one is worked on
+#pragma unroll
+        for (int u = 0; u < D - 1; ++u) load(b[u], wave + u * W);
+        for (int kb = wave; kb < n_kb; kb += D * W) {
+#pragma unroll
+            for (int u = 0; u < D; ++u) {
+                load(b[(u + D - 1) % D], kb + (u + D - 1) * W);
+                compute(b[u]);
+            }
+        }
     }
+    f32x4 *const s_part = (f32x4 *)s_mem;
+    if (W > 1) __syncthreads();       // (A's places are written over)
+    if (W > 1) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s_part[((wave * MT + m) * NT + t) * 64 + lane] = sum[m][t];
+        __syncthreads();
+    }
+    for (int tile = W > 1 ? wave : 0; tile < MT * NT; tile += W) {
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+        if (W > 1) {
+            for (int w = 0; w < W; ++w) y += s_part[(w * MT * NT + tile) * 64 + lane];
+        } else {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    if (m * NT + t == tile) y = sum[m][t];
+        }
+        const int nt = t0 + tile % NT, m_first = m0 + 16 * (tile / NT) + 4 * kg;
+        if (nt >= n_tiles) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int m = m_first + r;
+            if (g.epi == EPI_SWIGLU) {
+                const float up = __shfl_xor(y[r], 8, 64);
+                if (n15 < 8 && m < g.M)
+                    ((bf16 *)g.out)[(size_t)m * (g.N >> 1) + nt * 8 + n15] = __float2bfloat16(y[r] / (1.f + __expf(-y[r])) * up);
+            } else if (m < g.M) {
+                const size_t at = (size_t)m * g.N + nt * 16 + n15;
+                ((float *)g.out)[at] = g.epi == EPI_RESID_F32 ? g.resid[at] + y[r] : y[r];
+            }
+        }
+    }
+}
+
+template <int MT, int AL, int NT, int NG, int D>
+hipError_t launch_group(const W4Gemm &a, int W, hipStream_t s) {
+    const int n_mb = (a.M + 16 * MT - 1) / (16 * MT), n_nb = (a.N / 16 + NT - 1) / NT;
+    const size_t lds = (size_t)W * MT * 1024 * std::max(4, NT);        // rows of A, then partial sums
+    if (lds > 65536) {
+        static std::atomic<uint32_t> set{0};
+        if (hipError_t e = set_dynamic_lds_once(set, (const void *)w4_gemm_kernel<MT, AL, NT, NG, D>, max_waves(MT, NT) * MT * 1024 * std::max(4, NT))) return e;
+    }
+    w4_gemm_kernel<MT, AL, NT, NG, D><<<dim3((unsigned)n_mb * (unsigned)n_nb), dim3(64 * W), lds, s>>>(a, n_mb, W);
+    return hipGetLastError();
+}
+template <int MT, int AL, int NT, int D>
+hipError_t launch(const W4Gemm &a, int W, hipStream_t s) {
+    return a.group == 128 ? launch_group<MT, AL, NT, 1, D>(a, W, s) : a.group == 64 ? launch_group<MT, AL, NT, 2, D>(a, W, s) : launch_group<MT, AL, NT, 4, D>(a, W, s);
 }
 
 }  // namespace
@@ -85,10 +244,58 @@ hipError_t launch_w4_pack(const uint8_t *codes, const __half *scales, const __ha
     return hipGetLastError();
 }
 
+// Which rows of A and of W a workgroup takes, and how many wavefronts share its k.  Up to 16 rows the bytes of W bound the product:
+// 32 rows of W a workgroup once there are 256 tiles of 16 (N = 5120, K = 27648, 8 rows, groups of 64: 24 us, with 16 rows of W 29;
+// N = 1536, K = 8960, one row: 7.6, with 16 rows 5.6), wavefronts to about 2048 in all, each with at least one and a half blocks.
+// More rows are bound by the vector and matrix pipes: the tile with the least of w4_cost, in rounds of 256 workgroups.  Measured (us)
+// for 2x2, 2x4, 3x2, 3x4, 4x4 tiles of 16: 72 rows, N = 7168, K = 5120, groups of 128: 21.0, 19.9, 19.8, 16.2, 19.8;  48, 5120, 5120, 64:
+// 15.6, 14.4, 13.8, 17.9, -;  128, 1536, 8960, 128: 14.7, 18.3, 17.3, -, -;  128, 55296, 5120, 128: 166, 131, -, 139, 120.
+struct W4Tile { int mt, nt, W; };
+
+int w4_cost(int mt, int nt, int ng) {    // issue cycles of a wavefront's block, in vector instructions: rows of A; unpacking; sums and products
+    return mt * 46 + nt * 32 + mt * nt * (8 * ng + 8) + 40;
+}
+
+W4Tile w4_tile(int M, int N, int K, int group) {
+    const int tiles = N / 16, n_kb = w4_kblocks(K);
+    W4Tile t = {1, 1, 4};
+    long groups;
+    if (M <= 16) {
+        t.nt = tiles >= 256 ? 2 : 1;
+        groups = (tiles + t.nt - 1) / t.nt;
+        while (t.W < 16 && groups * t.W < 2048) t.W *= 2;
+    } else {
+        long best = -1;
+        for (const auto &c : {W4Tile{2, 2, 0}, W4Tile{2, 4, 0}, W4Tile{3, 2, 0}, W4Tile{3, 4, 0}, W4Tile{4, 4, 0}}) {
+            const long units = (long)((M + 16 * c.mt - 1) / (16 * c.mt)) * ((tiles + c.nt - 1) / c.nt);
+            const long cost = (units + 255) / 256 * w4_cost(c.mt, c.nt, 128 / group);
+            if (best < 0 || cost < best) {
+                best = cost;
+                t = c;
+                t.W = units <= 256 ? 8 : 4;
+            }
+        }
+    }
+    while (t.W > 4 && 2 * n_kb < 3 * t.W) t.W /= 2;
+    t.W = std::min(t.W, n_kb);
+    return t;
+}
+
 hipError_t launch_w4_gemm(const W4Gemm &a, hipStream_t s) {
-    const long n = (long)a.M * (a.epi == EPI_SWIGLU ? a.N / 2 : a.N);
-    w4_gemm_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(a);
-    return hipGetLastError();
+    W4Tile t = w4_tile(a.M, a.N, a.K, a.group);
+#ifdef W4_TUNE
+    if (getenv("W4_MT")) t.mt = atoi(getenv("W4_MT"));
+    if (getenv("W4_NT")) t.nt = atoi(getenv("W4_NT"));
+    if (getenv("W4_W")) t.W = std::min(std::min(atoi(getenv("W4_W")), w4_kblocks(a.K)), max_waves(t.mt, t.nt));
+    if (t.mt > 1 && t.nt < 2) t.nt = 2;
+    if (t.mt == 1 && t.nt > 2) t.nt = 2;
+#endif
+    if (t.mt == 1 && a.M <= 4) return t.nt == 1 ? launch<1, 1, 1, 2>(a, t.W, s) : launch<1, 1, 2, 2>(a, t.W, s);
+    if (t.mt == 1 && a.M <= 8) return t.nt == 1 ? launch<1, 2, 1, 2>(a, t.W, s) : launch<1, 2, 2, 2>(a, t.W, s);
+    if (t.mt == 1) return t.nt == 1 ? launch<1, 4, 1, 2>(a, t.W, s) : launch<1, 4, 2, 2>(a, t.W, s);
+    if (t.mt == 2) return t.nt == 2 ? launch<2, 8, 2, 1>(a, t.W, s) : launch<2, 8, 4, 1>(a, t.W, s);
+    if (t.mt == 3) return t.nt == 2 ? launch<3, 12, 2, 1>(a, t.W, s) : launch<3, 12, 4, 1>(a, t.W, s);
+    return launch<4, 16, 4, 1>(a, t.W, s);
 }
 
 }  // namespace cs
