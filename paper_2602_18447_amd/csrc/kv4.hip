@@ -9,14 +9,18 @@ namespace {
 
 __device__ __forceinline__ float bf16_f32(bf16 v) { return __bfloat162float(v); }
 
-// Trace of packed token t: the largest b with cu[b] <= t.
-__device__ __forceinline__ int trace_of(const int32_t *cu, int B, int t) {
-    int lo = 0, hi = B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (cu[mid] <= t) lo = mid; else hi = mid - 1;
+// Trace of packed token t, the largest b with cu[b] <= t, by a whole wavefront: 64 candidates a round instead of two (a round is a
+// trip to L2; a call on few tokens is made of such trips).
+__device__ __forceinline__ int trace_of(const int32_t *cu, int B, int t, int lane) {
+    int lo = 0, n = B;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, at = lane * step;
+        const int found = __popcll(__ballot(at < n && cu[min(lo + at, B - 1)] <= t));
+        const int skip = max(found - 1, 0) * step;
+        lo += skip;
+        n = min(step, n - skip);
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 // Page of cache row `row` of trace b and head h, clamped into the cache.
 __device__ __forceinline__ uint8_t *page_of(const Kv4Batch &b, int trace, int row, int h) {
@@ -60,73 +64,90 @@ __device__ __forceinline__ void sincos64(double x, double &s, double &c) {
     c = (quadrant == 1 || quadrant == 2) ? -b : b;
 }
 
-// One workgroup per token, a wavefront per head in turn; lane i has elements i and i + 64.
-__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a) {
+// Half a wavefront per head, eight heads a workgroup at a time, n_split workgroups per token; lane i of a half has elements 2 i, 2 i + 1
+// and the 64 further ones they are paired with.  Bound by the bytes of qkv and of q, k, v where tokens are many.
+__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_split) {
     const Kv4Batch &b = a.b;
-    const int t = blockIdx.x, lane = threadIdx.x & 63;
-    const int trace = trace_of(b.cu, b.B, t);
-    const int i = min(max(t - b.cu[trace], 0), b.T - 1), L = max(b.plens[trace], 0), row = L + i;
+    const int t = blockIdx.x / n_split, split = blockIdx.x % n_split, lane = threadIdx.x & 63, i2 = lane & 31, heads = a.Hq + 2 * b.Hkv;
+    int h = split * 8 + (threadIdx.x >> 5);
+    const float *src = a.qkv + (size_t)t * a.stride + 2 * i2;
+    float2 lo = *(const float2 *)(src + (size_t)min(h, heads - 1) * 128), hi = *(const float2 *)(src + (size_t)min(h, heads - 1) * 128 + 64);
+    const int trace = trace_of(b.cu, b.B, t, lane);
+    const int i = min(max(t - b.cu[trace], 0), b.T - 1), L = max(b.plens[trace], 0), row = L + i, slot = row & 15;
     const bool store = (!a.n_append || i < a.n_append[trace]) && row >= 0 && row < b.max_blocks * 16;
-    double sn, cn;
-    sincos64((double)row * a.inv_freq[lane], sn, cn);
-    for (int h = threadIdx.x >> 6; h < a.Hq + 2 * b.Hkv; h += 4) {
-        const float *src = a.qkv + (size_t)t * a.stride + (size_t)h * 128;
-        float lo = src[lane], hi = src[lane + 64];
-        if (h < a.Hq + b.Hkv) {
-            const double x = lo, y = hi;
-            lo = (float)(x * cn - y * sn);
-            hi = (float)(y * cn + x * sn);
+    uint8_t *const pages = page_of(b, trace, row, 0);
+    double s0, c0, s1, c1;
+    sincos64((double)row * a.inv_freq[2 * i2], s0, c0);
+    sincos64((double)row * a.inv_freq[2 * i2 + 1], s1, c1);
+    for (; h < heads; h += 8 * n_split) {
+        float2 lo_next = lo, hi_next = hi;
+        if (h + 8 * n_split < heads) {
+            lo_next = *(const float2 *)(src + (size_t)(h + 8 * n_split) * 128);
+            hi_next = *(const float2 *)(src + (size_t)(h + 8 * n_split) * 128 + 64);
         }
-        const bf16 l16 = __float2bfloat16(lo), h16 = __float2bfloat16(hi);
+        if (h < a.Hq + b.Hkv) {
+            const double x0 = lo.x, x1 = lo.y, y0 = hi.x, y1 = hi.y;
+            lo = make_float2((float)(x0 * c0 - y0 * s0), (float)(x1 * c1 - y1 * s1));
+            hi = make_float2((float)(y0 * c0 + x0 * s0), (float)(y1 * c1 + x1 * s1));
+        }
+        const bf16 r[4] = {__float2bfloat16(lo.x), __float2bfloat16(lo.y), __float2bfloat16(hi.x), __float2bfloat16(hi.y)};
         const bool is_k = h >= a.Hq && h < a.Hq + b.Hkv;
         const int hk = is_k ? h - a.Hq : h - a.Hq - b.Hkv;
-        bf16 *dst = h < a.Hq ? a.q + ((size_t)t * a.Hq + h) * 128 : (is_k ? a.k : a.v) + ((size_t)t * b.Hkv + hk) * 128;
-        dst[lane] = l16;
-        dst[lane + 64] = h16;
-        if (h < a.Hq || !store) continue;
-        // min and max of the row, its pair (s, z), the codes
-        const float x0 = __builtin_amdgcn_fmed3f(bf16_f32(l16), -65504.f, 65504.f), x1 = __builtin_amdgcn_fmed3f(bf16_f32(h16), -65504.f, 65504.f);
-        float mn = fminf(x0, x1), mx = fmaxf(x0, x1);
+        bf16 *dst = (h < a.Hq ? a.q + ((size_t)t * a.Hq + h) * 128 : (is_k ? a.k : a.v) + ((size_t)t * b.Hkv + hk) * 128) + 2 * i2;
+        *(unsigned *)dst = (unsigned)__bfloat16_as_ushort(r[0]) | (unsigned)__bfloat16_as_ushort(r[1]) << 16;
+        *(unsigned *)(dst + 64) = (unsigned)__bfloat16_as_ushort(r[2]) | (unsigned)__bfloat16_as_ushort(r[3]) << 16;
+        if (h >= a.Hq && store) {
+            // min and max of the row, its pair (s, z), the codes
+            float x[4];
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) { mn = fminf(mn, __shfl_xor(mn, o, 64)); mx = fmaxf(mx, __shfl_xor(mx, o, 64)); }
-        const __half zh = __float2half_rn(mn + 0.f);            // (never -0)
-        const float z = __half2float(zh);
-        const __half sh = __float2half_rn((float)(((double)mx - (double)z) / 15.0) + 0.f);
-        const float s = __half2float(sh);
-        const float c0 = s > 0.f ? fminf(fmaxf(rintf((x0 - z) / s), 0.f), 15.f) : 0.f;
-        const float c1 = s > 0.f ? fminf(fmaxf(rintf((x1 - z) / s), 0.f), 15.f) : 0.f;
-        const int e = lane & 7, sft = is_k ? k_shift(e) : 4 * e;
-        unsigned w0 = (unsigned)c0 << sft, w1 = (unsigned)c1 << sft;
+            for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_fmed3f(bf16_f32(r[e]), -65504.f, 65504.f);
+            float mn = fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) { w0 |= __shfl_xor((int)w0, o, 64); w1 |= __shfl_xor((int)w1, o, 64); }
-        uint8_t *page = page_of(b, trace, row, hk);
-        const int slot = row & 15;
-        if (e == 0) {
-            *(unsigned *)(page + (is_k ? k_word(slot, lane) : v_word(slot, lane))) = w0;
-            *(unsigned *)(page + (is_k ? k_word(slot, lane + 64) : v_word(slot, lane + 64))) = w1;
+            for (int o = 16; o > 0; o >>= 1) { mn = fminf(mn, __shfl_xor(mn, o, 64)); mx = fmaxf(mx, __shfl_xor(mx, o, 64)); }
+            const __half zh = __float2half_rn(mn + 0.f);            // (never -0)
+            const float z = __half2float(zh);
+            const __half sh = __float2half_rn((float)(((double)mx - (double)z) / 15.0) + 0.f);
+            const float s = __half2float(sh);
+            unsigned c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = s > 0.f ? (unsigned)fminf(fmaxf(rintf((x[e] - z) / s), 0.f), 15.f) : 0u;
+            const int e = 2 * (lane & 3);                           // place of the first of the lane's two in their word of eight
+            unsigned w0 = is_k ? c[0] << k_shift(e) | c[1] << k_shift(e + 1) : (c[0] | c[1] << 4) << (4 * e);
+            unsigned w1 = is_k ? c[2] << k_shift(e) | c[3] << k_shift(e + 1) : (c[2] | c[3] << 4) << (4 * e);
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) { w0 |= (unsigned)__shfl_xor((int)w0, o, 64); w1 |= (unsigned)__shfl_xor((int)w1, o, 64); }
+            uint8_t *page = pages + (size_t)hk * KV4_PAGE;
+            if (e == 0) {
+                *(unsigned *)(page + (is_k ? k_word(slot, 2 * i2) : v_word(slot, 2 * i2))) = w0;
+                *(unsigned *)(page + (is_k ? k_word(slot, 2 * i2 + 64) : v_word(slot, 2 * i2 + 64))) = w1;
+            }
+            if (i2 == 0)
+                *(unsigned *)(page + (is_k ? KV4_KP : KV4_VP) + slot * 4) = (unsigned)__half_as_ushort(sh) | (unsigned)__half_as_ushort(zh) << 16;
         }
-        if (lane == 0)
-            *(unsigned *)(page + (is_k ? KV4_KP : KV4_VP) + slot * 4) = (unsigned)__half_as_ushort(sh) | (unsigned)__half_as_ushort(zh) << 16;
+        lo = lo_next;
+        hi = hi_next;
     }
 }
 
 __device__ __forceinline__ float param_s(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p & 0xffff))); }
 __device__ __forceinline__ float param_z(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p >> 16))); }
 
-// One workgroup per token; a thread has 8 elements (one word) of a key or value row.
-__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, float *__restrict__ k, float *__restrict__ v) {
-    const int t = blockIdx.x;
-    const int trace = trace_of(b.cu, b.B, t);
+// A thread has 8 elements (one word) of a key or value row; eight heads of a token a workgroup.
+__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, float *__restrict__ k, float *__restrict__ v) {
+    const int t = blockIdx.x / n_split, h = blockIdx.x % n_split * 8 + (threadIdx.x >> 5);
+    const int trace = trace_of(b.cu, b.B, t, threadIdx.x & 63);
     const int row = max(b.plens[trace], 0) + min(max(t - b.cu[trace], 0), b.T - 1), slot = row & 15;
-    for (int j = threadIdx.x; j < b.Hkv * 32; j += 256) {
-        const int h = j >> 5, is_v = (j >> 4) & 1, d = (j & 15) * 8;
-        const uint8_t *page = page_of(b, trace, row, h);
-        const unsigned w = *(const unsigned *)(page + (is_v ? v_word(slot, d) : k_word(slot, d)));
-        const unsigned p = *(const unsigned *)(page + (is_v ? KV4_VP : KV4_KP) + slot * 4);
-        float *dst = (is_v ? v : k) + ((size_t)t * b.Hkv + h) * 128 + d;
+    if (h >= b.Hkv) return;
+    const int is_v = (threadIdx.x >> 4) & 1, d = (threadIdx.x & 15) * 8;
+    const uint8_t *page = page_of(b, trace, row, h);
+    const unsigned w = *(const unsigned *)(page + (is_v ? v_word(slot, d) : k_word(slot, d)));
+    const unsigned p = *(const unsigned *)(page + (is_v ? KV4_VP : KV4_KP) + slot * 4);
+    float *dst = (is_v ? v : k) + ((size_t)t * b.Hkv + h) * 128 + d;
+    float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dst[e] = fmaf(param_s(p), (float)((w >> (is_v ? 4 * e : k_shift(e))) & 15), param_z(p));
-    }
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(param_s(p), (float)((w >> (is_v ? 4 * e : k_shift(e))) & 15), param_z(p));
+    *(float4 *)dst = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4 *)(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
 // ---- attention ----
@@ -136,8 +157,8 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, float *__rest
 // wavefronts until the end and keeps its own (maximum, sum, O).
 //  * Scores S^T = K Q^T: a page's key codes are the first operand of four 16x16x32 products as they lie in memory, 16
 //    bytes a lane; code c enters as the bfloat16 16 + c (the code's four bits put into the mantissa of 16), which is
-//    exact, and the sum starts at -24 sum(q), so that it ends as sum q (c - 8).  A lane then has four keys of one query row:
-//    score = s sum + (z + 8 s) sum(q).
+//    exact, and the sum starts at -16 sum(q), so that it ends as sum q c.  A lane then has four keys of one query row:
+//    score = s sum + z sum(q), two multiply-adds that take s and z as the halves they are.
 //  * O^T = V^T P^T: the lane's four keys of both pages are the eight consecutive k of the second operand as they are, and
 //    a page's value codes lie in memory such that a lane's 16 bytes are those four tokens of eight columns.  Code c
 //    enters as the half c 2^-24 (its four bits alone), the probability as the half p s; z is added to the row's sum.
@@ -168,8 +189,15 @@ __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __built
 __device__ __forceinline__ unsigned lo_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }   // b.lo : a.lo
 __device__ __forceinline__ unsigned hi_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 // Eight key codes as bfloat16 16 + c: element 2 k and 2 k + 1 are nibbles k and k + 4.
-__device__ __forceinline__ bf16x8 key_codes(unsigned w) {
-    constexpr unsigned M = 0x00780078u, C = 0x41804180u;
+struct CodeBits { unsigned mask, one; };   // in registers: one and-or takes both only if neither is a literal
+__device__ __forceinline__ CodeBits code_bits() {
+    CodeBits b;
+    asm("s_mov_b32 %0, 0x780078" : "=s"(b.mask));
+    asm("v_mov_b32 %0, 0x41804180" : "=v"(b.one));
+    return b;
+}
+__device__ __forceinline__ bf16x8 key_codes(unsigned w, CodeBits b) {
+    const unsigned M = b.mask, C = b.one;
     const u32x4 r = {((w << 3) & M) | C, ((w >> 1) & M) | C, ((w >> 5) & M) | C, ((w >> 9) & M) | C};
     return __builtin_bit_cast(bf16x8, r);
 }
@@ -191,9 +219,17 @@ __device__ __forceinline__ float sum_over_g(float v) {
 }
 
 constexpr float SCALE_LOG2 = 0.08838834764831845f * 1.4426950408889634f;
-constexpr float M_NONE = -1e30f;      // reference of a row that has seen no key
-constexpr float M_ROOM = 8.f;         // p s may exceed 2^5 by this power of two: below 2^14, a half ends at 2^16
+// References: M bounds score + exponent field of s (15 where s is 1), all in powers of two; p = 2^(score - M + REF).
+// Then p s < 2^(M_ROOM + 6) = 2^14 whatever the rows' s are, and a half ends at 2^16; p itself stays below 2^(M_ROOM + REF).
+constexpr float M_NONE = -1e30f, M_ROOM = 8.f, REF = 20.f, E_ONE = 15.f;
 constexpr float V_UNIT = 1.f / 16777216.f;
+
+// Loads of 16 bytes from a wave-uniform base plus a byte offset per lane; offsets at or past the end read zeros.
+struct Loads {
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ Loads(const void *base, unsigned bytes) : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00020000)) {}
+    __device__ u32x4 get(unsigned off) const { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)off, 0, 0)); }
+};
 
 // What a wavefront needs of two pages; a lane's part of the pairs (s, z) are those of its four keys.
 struct Chunk4 {
@@ -203,7 +239,7 @@ struct Chunk4 {
 template <int NQ>
 struct Rows4 {                        // state of a wavefront's rows: a lane has row lane % 16 of each 16
     bf16x8 q[NQ][4];
-    f32x4 q_off[NQ];                  // -24 sum(q), four times
+    f32x4 q_off[NQ];                  // -16 sum(q), four times
     float q_sum[NQ], m[NQ], l[NQ], zs[NQ];
     f32x4 o[NQ][8];                   // [j][r]: column 32 (lane / 16) + 8 r + j, in units of 2^-24
 };
@@ -226,58 +262,63 @@ __device__ __forceinline__ void raise(Rows4<NQ> &R, const float (&t_max)[NQ]) {
     }
 }
 
-// 32 cached tokens, of which the first n_valid count.
+__device__ __forceinline__ float mix(unsigned p, float a, float b) { return fmaf((float)__builtin_bit_cast(f16x2, p)[0], a, b); }    // s a + b
+__device__ __forceinline__ float mix_z(unsigned p, float a, float b) { return fmaf((float)__builtin_bit_cast(f16x2, p)[1], a, b); }
+
+// 32 cached tokens, of which the first n_valid count; what is stored for the others may be anything.
 template <int NQ>
-__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g) {
+__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g, CodeBits bits) {
     f32x4 sc[NQ][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const bf16x8 a = key_codes(c.k[x][i]);
+            const bf16x8 a = key_codes(c.k[x][i], bits);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) sc[n][x] = mma(a, R.q[n][i], i == 0 ? R.q_off[n] : sc[n][x]);
         }
-    float vs[2][4], vz[2][4], t_max[NQ];
+    u32x4 vp[2] = {c.vp[0], c.vp[1]};
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) sc[n][x][r] = mix(c.kp[x][r], sc[n][x][r], mix_z(c.kp[x][r], R.q_sum[n], 0.f));
+    if (n_valid < 32)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * x + 4 * g + r >= n_valid) {
+                    vp[x][r] = 0u;
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) sc[n][x][r] = -INFINITY;
+                }
+    float t_max[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) t_max[n] = -INFINITY;
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            float ks = param_s(c.kp[x][r]) * SCALE_LOG2, kz = param_z(c.kp[x][r]) * SCALE_LOG2;
-            vs[x][r] = param_s(c.vp[x][r]);
-            vz[x][r] = param_z(c.vp[x][r]);
-            const bool valid = 16 * x + 4 * g + r < n_valid;
-            if (n_valid < 32 && !valid) vs[x][r] = vz[x][r] = 0.f;
-            const float e = (float)max((__float_as_uint(vs[x][r]) >> 23) & 255u, 103u);     // exponent of s, biased by 127; of 2^-24 at least
-            kz = fmaf(8.f, ks, kz);
+            const float e = (float)((vp[x][r] >> 10) & 31u);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                float s = fmaf(ks, sc[n][x][r], kz * R.q_sum[n]);
-                if (n_valid < 32) s = valid ? s : -INFINITY;
-                sc[n][x][r] = s;
-                t_max[n] = fmaxf(t_max[n], s + e);
-            }
+            for (int n = 0; n < NQ; ++n) t_max[n] = fmaxf(t_max[n], fmaf(sc[n][x][r], SCALE_LOG2, e));
         }
     raise<NQ>(R, t_max);
     f16x8 w[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        const float ref = R.m[n] - 132.f;
-        u32x4 pk;
+        const float ref = REF - R.m[n];
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int r = 0; r < 4; r += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(sc[n][x][r] - ref), p1 = __builtin_amdgcn_exp2f(sc[n][x][r + 1] - ref);
-                R.l[n] += p0;
-                R.l[n] += p1;
-                R.zs[n] = fmaf(p0, vz[x][r], R.zs[n]);
-                R.zs[n] = fmaf(p1, vz[x][r + 1], R.zs[n]);
-                pk[2 * x + (r >> 1)] = pack_f16(p0 * vs[x][r], p1 * vs[x][r + 1]);
+            for (int r = 0; r < 4; ++r) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[n][x][r], SCALE_LOG2, ref));
+                R.l[n] += p;
+                R.zs[n] = mix_z(vp[x][r], p, R.zs[n]);
+                w[n][4 * x + r] = (_Float16)mix(vp[x][r], p, 0.f);
             }
-        w[n] = __builtin_bit_cast(f16x8, pk);
     }
     unsigned lo[4], hi[4];
 #pragma unroll
@@ -297,12 +338,11 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
     }
 }
 
-__device__ __forceinline__ bool any_not_finite(unsigned w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
-
 // 32 suffix tokens from j0 on; k, v point at the trace's first token and the head, rows are `stride` elements apart; a row
-// sees tokens up to its own (tok).  Products in bfloat16, probabilities in two terms.
+// sees tokens up to its own (tok).  Products in bfloat16, probabilities in two terms.  True: values were taken out that
+// add_not_finite has to add.
 template <int NQ>
-__device__ __forceinline__ void suffix_chunk(Rows4<NQ> &R, const bf16 *k, const bf16 *v, size_t stride, int j0, int S, const int (&tok)[NQ],
+__device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *k, const bf16 *v, size_t stride, int j0, int S, const int (&tok)[NQ],
                                              int n15, int g) {
     f32x4 sc[NQ][2];
 #pragma unroll
@@ -334,19 +374,38 @@ __device__ __forceinline__ void suffix_chunk(Rows4<NQ> &R, const bf16 *k, const 
             for (int r = 0; r < 4; ++r) {
                 const float s = j0 + 16 * x + 4 * g + r <= tok[n] ? sc[n][x][r] * SCALE_LOG2 : -INFINITY;
                 sc[n][x][r] = s;
-                t_max[n] = fmaxf(t_max[n], s + 127.f);
+                t_max[n] = fmaxf(t_max[n], s + E_ONE);
             }
+    }
+    // A value that is not a finite number may only reach the rows that see its token, but a product takes 0 times it into every
+    // row: where rows see a part of the tokens, such values are taken out.
+    bool bad = false;
+    if (__any(masked)) {
+        unsigned any = 0;
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) any |= (vw[t][e] & 0x7fff7fffu) + 0x00800080u;      // a full exponent carries into the sign's place
+        bad = __any((any & 0x80008000u) != 0u);
+        if (bad)
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if ((vw[t][e] & 0x7f80u) == 0x7f80u) vw[t][e] &= 0xffff0000u;
+                    if ((vw[t][e] & 0x7f800000u) == 0x7f800000u) vw[t][e] &= 0xffffu;
+                }
     }
     raise<NQ>(R, t_max);
     u32x4 hi[NQ], lo[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        const float ref = R.m[n] - 132.f;
+        const float ref = REF - R.m[n];
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 4; r += 2) {
-                float p0 = __builtin_amdgcn_exp2f(sc[n][x][r] - ref), p1 = __builtin_amdgcn_exp2f(sc[n][x][r + 1] - ref);
+                float p0 = __builtin_amdgcn_exp2f(sc[n][x][r] + ref), p1 = __builtin_amdgcn_exp2f(sc[n][x][r + 1] + ref);
                 R.l[n] += p0;
                 R.l[n] += p1;
                 p0 *= V_UNIT;
@@ -357,42 +416,6 @@ __device__ __forceinline__ void suffix_chunk(Rows4<NQ> &R, const bf16 *k, const 
                 hi[n][2 * x + (r >> 1)] = h;
                 lo[n][2 * x + (r >> 1)] = pack_bf16(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
             }
-    }
-    // A value that is not a finite number may only reach the rows that see its token, but the matrix product takes 0 times
-    // it into every row: such values are taken out and added one by one where they are seen.
-    if (__any(masked)) {
-        bool bad = false;
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) bad |= any_not_finite(vw[t][e]);
-        if (__any(bad)) {
-#pragma unroll
-            for (int t = 0; t < 8; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if ((vw[t][e] & 0x7f80u) == 0x7f80u) vw[t][e] &= 0xffff0000u;
-                    if ((vw[t][e] & 0x7f800000u) == 0x7f800000u) vw[t][e] &= 0xffffu;
-                }
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    for (int g2 = 0; g2 < 4; ++g2) {
-                        const int j = j0 + 16 * x + 4 * g2 + r;
-                        if (j >= S) continue;
-                        const unsigned short *row = (const unsigned short *)(v + (size_t)j * stride + 32 * g);
-#pragma unroll
-                        for (int n = 0; n < NQ; ++n) {
-                            const float p = __shfl(sc[n][x][r], n15 + 16 * g2, 64);
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) {
-                                const unsigned bits = row[c];
-                                if ((bits & 0x7f80u) == 0x7f80u && j <= tok[n]) R.o[n][c & 7][c >> 3] += p * __uint_as_float(bits << 16);
-                            }
-                        }
-                    }
-        }
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -405,6 +428,28 @@ __device__ __forceinline__ void suffix_chunk(Rows4<NQ> &R, const bf16 *k, const 
         for (int n = 0; n < NQ; ++n) {
             R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, hi[n]), R.o[n][j]);
             R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, lo[n]), R.o[n][j]);
+        }
+    }
+    return bad;
+}
+
+// Adds the values that suffix_chunk took out of tokens j_begin .. j_end - 1 to the rows that see them.  A probability is positive,
+// so that an infinity or NaN is what its column becomes, whatever the probability.
+template <int NQ>
+__device__ __forceinline__ void add_not_finite(Rows4<NQ> &R, const bf16 *v, size_t stride, int j_begin, int j_end, const int (&tok)[NQ], int g) {
+#pragma unroll 1
+    for (int j = j_begin; j < j_end; ++j) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const u32x4 w = *(const u32x4 *)(v + (size_t)j * stride + 32 * g + 8 * r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const unsigned bits = e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16;
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+                    if ((bits & 0x7f800000u) == 0x7f800000u && j <= tok[n]) R.o[n][e][r] += __uint_as_float(bits);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
@@ -458,7 +503,7 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 ? 3 : 2) void kv4_attn_kernel
             for (int e = 0; e < 8; ++e) sum += (float)R.q[n][i][e];
         }
         R.q_sum[n] = sum_over_g(sum);
-        R.q_off[n] = f32x4{1.f, 1.f, 1.f, 1.f} * (-24.f * R.q_sum[n]);
+        R.q_off[n] = f32x4{1.f, 1.f, 1.f, 1.f} * (-16.f * R.q_sum[n]);
         R.m[n] = M_NONE;
         R.l[n] = R.zs[n] = 0.f;
 #pragma unroll
@@ -468,49 +513,61 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 ? 3 : 2) void kv4_attn_kernel
     // chunks of this piece: cached ones first, then the suffix as far as the tile's last row sees it
     const int n_cached = (L + 31) >> 5, tok_hi = (min((rt + 1) * ROWS, n_rows) - 1) / G, n_all = n_cached + (tok_hi >> 5) + 1;
     const int c_begin = (int)((int64_t)n_all * piece / P), c_end = (int)((int64_t)n_all * (piece + 1) / P);
-    int c = c_begin + wk;
     const int c_stop = min(c_end, n_cached);
-    if (c < c_stop) {
+    if (c_begin + wk < c_stop) {
         const int32_t *table = kv.table + (size_t)trace * kv.max_blocks;
         const uint8_t *head = kv.pages + (size_t)h * KV4_PAGE;
         const size_t block_bytes = (size_t)kv.Hkv * KV4_PAGE;
-        const unsigned at16 = lane * 16, at_g = g * 16;
-        int ids = 0, left = 0;        // block numbers of the next 32 chunks, two lanes each
-        auto load = [&](Chunk4 &d, int cc) {
-            if (left == 0) {
-                const int page = 2 * (cc + WK * (lane >> 1)) + (lane & 1);
-                ids = min(max(table[min(page, kv.max_blocks - 1)], 0), kv.n_blocks - 1);
-                left = 32;
-            }
+        const unsigned at16 = lane * 16, at_kp = KV4_KP + g * 16;
+        const CodeBits bits = code_bits();
+        // Block numbers of 32 chunks, two lanes each, and of the 32 after them; chunk i of this wavefront is c_begin + wk + i WK.
+        auto block_ids = [&](int i0) {
+            const int page = 2 * (c_begin + wk + WK * (i0 + (lane >> 1))) + (lane & 1);
+            return table[min(page, kv.max_blocks - 1)];
+        };
+        int ids = block_ids(0), ids_next = block_ids(32);
+        auto load = [&](Chunk4 &d, int i) {      // (a chunk behind the last one reads zeros, and touches no memory)
+            const unsigned bytes = c_begin + wk + WK * i < c_stop ? KV4_PAGE : 0;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const uint8_t *page = head + (size_t)__builtin_amdgcn_readlane(ids, 2 * (32 - left) + x) * block_bytes;
-                d.k[x] = *(const u32x4 *)(page + at16);
-                d.v[x] = *(const u32x4 *)(page + KV4_V + at16);
-                d.kp[x] = *(const u32x4 *)(page + KV4_KP + at_g);
-                d.vp[x] = *(const u32x4 *)(page + KV4_VP + at_g);
+                const int id = min(max(__builtin_amdgcn_readlane((i & 31) == 0 && i ? ids_next : ids, 2 * (i & 31) + x), 0), kv.n_blocks - 1);
+                const Loads page(head + (size_t)id * block_bytes, bytes);
+                d.k[x] = page.get(at16);
+                d.v[x] = page.get(KV4_V + at16);
+                d.kp[x] = page.get(at_kp);
+                d.vp[x] = page.get(KV4_VP - KV4_KP + at_kp);
             }
-            --left;
+            __builtin_amdgcn_sched_barrier(0);   // (loads stay ahead of the products before them in time)
         };
+        auto compute = [&](const Chunk4 &d, int i) {
+            cached_chunk<NQ>(R, d, L - 32 * (c_begin + wk + WK * i), g, bits);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        const int n = (c_stop - c_begin - wk + WK - 1) / WK;
         Chunk4 c0, c1;
-        load(c0, c);
-        for (;;) {
-            if (c + WK < c_stop) load(c1, c + WK);
-            cached_chunk<NQ>(R, c0, L - 32 * c, g);
-            c += WK;
-            if (c >= c_stop) break;
-            if (c + WK < c_stop) load(c0, c + WK);
-            cached_chunk<NQ>(R, c1, L - 32 * c, g);
-            c += WK;
-            if (c >= c_stop) break;
+        load(c0, 0);
+        for (int i = 0; i < n; i += 2) {
+            load(c1, i + 1);
+            compute(c0, i);
+            if ((i & 31) == 30) {                // the next 32 chunks' numbers are in use from here on
+                ids = ids_next;
+                ids_next = block_ids(i + 34);
+            }
+            load(c0, i + 2);
+            if (i + 1 < n) compute(c1, i + 1);
         }
     }
+    int c = c_begin + wk;
+    if (c < c_stop) c += (c_stop - c + WK - 1) / WK * WK;
     if (c_end > n_cached) {
         const size_t stride = (size_t)kv.Hkv * 128;
         const bf16 *k = a.k + (size_t)t0 * stride + (size_t)h * 128, *v = a.v + (size_t)t0 * stride + (size_t)h * 128;
         const int my_hi = (min(row0 + 16 * NQ, n_rows) - 1) / G;      // (negative rows cannot be: row0 may lie behind the last row)
-        for (; c < c_end; c += WK)
-            if (32 * (c - n_cached) <= my_hi) suffix_chunk<NQ>(R, k, v, stride, 32 * (c - n_cached), S, tok, n15, g);
+        for (; c < c_end; c += WK) {
+            const int j0 = 32 * (c - n_cached);
+            if (j0 > my_hi || !suffix_chunk<NQ>(R, k, v, stride, j0, S, tok, n15, g)) continue;
+            add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
+        }
     }
 
     const bool direct = P == 1;
@@ -649,12 +706,15 @@ void plan_launch(Launch4 &p, const int32_t *h_cu, const int32_t *h_lens, int b0,
 }  // namespace
 
 hipError_t launch_kv4_append(const Kv4Append &a, hipStream_t s) {
-    kv4_append_kernel<<<a.b.T, 256, 0, s>>>(a);
+    // (workgroups for the chip to fill, as far as there are heads; each takes the token's angles anew)
+    const int n_split = std::min((a.Hq + 2 * a.b.Hkv + 7) / 8, std::max(1, 1024 / a.b.T));
+    kv4_append_kernel<<<(unsigned)a.b.T * n_split, 256, 0, s>>>(a, n_split);
     return hipGetLastError();
 }
 
 hipError_t launch_kv4_read(const Kv4Batch &b, float *k, float *v, hipStream_t s) {
-    kv4_read_kernel<<<b.T, 256, 0, s>>>(b, k, v);
+    const int n_split = (b.Hkv + 7) / 8;
+    kv4_read_kernel<<<(unsigned)b.T * n_split, 256, 0, s>>>(b, n_split, k, v);
     return hipGetLastError();
 }
 

@@ -378,6 +378,34 @@ def test_attention_a_nan_stays_in_its_head():
     assert torch.equal(out[keep], good[keep])
 
 
+@pytest.mark.parametrize("Hq, Hkv, S", [(4, 2, 5), (6, 1, 40), (40, 8, 33), (12, 2, 100)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_attention_what_a_later_token_holds_stays_out(Hq, Hkv, S, bad):
+    """Keys and values of a suffix token that are not finite reach the rows from that token on, and no other."""
+    gen = _gen(41)
+    c = Cache(gen, Hkv, (50, 3), (S, 2))
+    q = torch.randn(c.T, Hq, 128, generator=gen, device=DEV).bfloat16()
+    k = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV).bfloat16()
+    v = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV).bfloat16()
+    at = S // 2
+    for name in ("v", "k"):
+        kk, vv = k.clone(), v.clone()
+        with Ctx(Hq, Hkv) as ctx:
+            good = _attn_check(ctx, c, Hq, Hkv, q, kk, vv).view(c.T, Hq, 128)
+            if name == "v":
+                vv[at, Hkv - 1, 77] = bad
+            else:
+                kk[at, Hkv - 1, 77] = float("nan")
+            out = torch.empty(c.T, Hq * 128, dtype=torch.bfloat16, device=DEV)
+            cb.confspec_op_kv4_attention(ctx, c.kv, c.batch, 0, q, kk, vv, out, c.scratch(ctx))
+            torch.cuda.synchronize()
+        out, G = out.view(c.T, Hq, 128), Hq // Hkv
+        seen = torch.zeros(c.T, Hq, 128, dtype=torch.bool, device=DEV)
+        seen[at:S, (Hkv - 1) * G:, slice(77, 78) if name == "v" else slice(None)] = True
+        assert torch.equal(out[~seen], good[~seen])
+        assert not bool(torch.isfinite(out[seen]).any())
+
+
 def test_cache_beyond_4_gib():
     """Pages whose byte offsets pass 32 bits."""
     Hq, Hkv = 4, 2
