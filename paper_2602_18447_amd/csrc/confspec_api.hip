@@ -1367,7 +1367,7 @@ int confspec_op_kv4_append(confspec_ctx *ctx, const confspec_kv4 *kv, const conf
     a.n_append = dev_n_append;
     a.q = (cs::bf16 *)dev_q; a.k = (cs::bf16 *)dev_k; a.v = (cs::bf16 *)dev_v;
     a.Hq = c.n_q_heads;
-    for (int i = 0; i < 64; ++i) a.inv_freq[i] = std::pow((double)c.rope_theta, -2.0 * i / 128.0);
+    for (int k = 0; k < 6; ++k) a.theta_pow[k] = std::pow((double)c.rope_theta, -(1 << k) / 64.0);
     if ((rc = check_device(ctx))) return rc;
     HIP_TRY(cs::launch_kv4_append(a, (hipStream_t)stream));
     return CONFSPEC_OK;

@@ -340,7 +340,7 @@ struct Kv4Append {
     const int32_t *n_append;  // null: all tokens
     bf16 *q, *k, *v;
     int32_t Hq;
-    double inv_freq[64];
+    double theta_pow[6];      // theta^(-2^k / 64)
 };
 hipError_t launch_kv4_append(const Kv4Append &a, hipStream_t s);
 hipError_t launch_kv4_read(const Kv4Batch &b, float *k, float *v, hipStream_t s);

@@ -2,6 +2,10 @@
 // confspec_int4.h.
 #include "kernels.h"
 #include <algorithm>
+#ifdef KV4_TUNE
+#include <cstdlib>
+#include <cstdio>
+#endif
 
 namespace cs {
 
@@ -76,9 +80,13 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
     const int i = min(max(t - b.cu[trace], 0), b.T - 1), L = max(b.plens[trace], 0), row = L + i, slot = row & 15;
     const bool store = (!a.n_append || i < a.n_append[trace]) && row >= 0 && row < b.max_blocks * 16;
     uint8_t *const pages = page_of(b, trace, row, 0);
+    // theta^(-j / 64) for j = 2 i and 2 i + 1, from its six powers of two (64 values in the arguments would be 2 us away, in host memory)
+    double f0 = i2 & 1 ? a.theta_pow[1] : 1.0;
+#pragma unroll
+    for (int k = 1; k < 5; ++k) f0 *= (i2 >> k) & 1 ? a.theta_pow[k + 1] : 1.0;
     double s0, c0, s1, c1;
-    sincos64((double)row * a.inv_freq[2 * i2], s0, c0);
-    sincos64((double)row * a.inv_freq[2 * i2 + 1], s1, c1);
+    sincos64((double)row * f0, s0, c0);
+    sincos64((double)row * (f0 * a.theta_pow[0]), s1, c1);
     for (; h < heads; h += 8 * n_split) {
         float2 lo_next = lo, hi_next = hi;
         if (h + 8 * n_split < heads) {
@@ -167,13 +175,11 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, 
 //    and what was summed scaled, only where a row goes beyond it by more than 2^8.
 //
 // Bound by the cache's bytes when rows are few (136 bytes a token and head), by the vector pipe when they are many.
-constexpr int ATT_TRACES = 256;       // traces of one launch: its plan travels in the kernel's arguments
+constexpr int ATT_TRACES = 256;       // traces of one launch
 struct AttnPlan4 {
-    int32_t b0, n_items, n_merge_rows, swizzle;
-    uint32_t start[ATT_TRACES + 1];   // first item of a trace
-    uint32_t part[ATT_TRACES];        // first partial record of a trace (cut into pieces[] > 1)
-    uint32_t mrow[ATT_TRACES + 1];    // first (head, row) of a trace for the merge
-    uint16_t pieces[ATT_TRACES];
+    int32_t b0, nb, per_log2;         // traces; chunks of keys of a piece at most, a power of two
+    int32_t n_items, n_records, n_merge_rows;
+    int32_t swizzle;
 };
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
@@ -454,20 +460,66 @@ __device__ __forceinline__ void add_not_finite(Rows4<NQ> &R, const bf16 *v, size
     }
 }
 
-// Trace of an item (entries of `start` behind the last trace are n_items).
-__device__ __forceinline__ int plan_trace(const uint32_t *start, unsigned item, int lane) {
-    int b = 0;
-#pragma unroll
-    for (int k = 0; k < ATT_TRACES / 64; ++k) b += __popcll(__ballot(start[1 + lane + 64 * k] <= item));
-    return __builtin_amdgcn_readfirstlane(min(b, ATT_TRACES - 1));
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xf, false); }
+__device__ __forceinline__ int scan64(int v) {               // inclusive sums over the lanes
+    v = dpp_add<0x111, 0xf>(v);                              // row_shr:1, 2, 4, 8 inside each 16 lanes
+    v = dpp_add<0x112, 0xf>(v);
+    v = dpp_add<0x114, 0xf>(v);
+    v = dpp_add<0x118, 0xf>(v);
+    v = dpp_add<0x142, 0xa>(v);                              // row_bcast:15, row_bcast:31
+    return dpp_add<0x143, 0xc>(v);
+}
+
+// Where an item of the launch (MERGE: a row of a trace that was cut) lies.  The list is never written out: every wavefront adds the
+// traces' counts up, 64 at a time, from the lengths it needs anyway - a list in the kernel's arguments cost 3 us, which lie in host
+// memory.  What the host counted (same arithmetic: count_items) bounds what is found.
+struct Place4 {
+    int trace, t0, S, L, P, n_tiles, local, first_record;
+    bool found;
+};
+struct Count4 { int tiles, pieces, items, records, merge_rows; };
+__host__ __device__ inline Count4 count_items(int L, int S, int G, int Hkv, int rows_log2, int per_log2) {
+    Count4 c;
+    c.tiles = (int)(((long)G * S + (1 << rows_log2) - 1) >> rows_log2);
+    c.pieces = (((L + 31) >> 5) + ((S + 31) >> 5) + (1 << per_log2) - 1) >> per_log2;
+    c.items = Hkv * c.tiles * c.pieces;
+    c.records = c.pieces > 1 ? c.items : 0;
+    c.merge_rows = c.pieces > 1 ? Hkv * G * S : 0;
+    return c;
+}
+template <bool MERGE>
+__device__ __forceinline__ Place4 find_item(const Kv4Batch &kv, const AttnPlan4 &plan, int G, int rows_log2, unsigned item, int lane) {
+    int items0 = 0, records0 = 0;
+    Place4 f = {};
+    for (int k = 0; k < plan.nb; k += 64) {
+        const int b = min(plan.b0 + min(k + lane, plan.nb - 1), kv.B - 1);
+        const int c0 = kv.cu[b], c1 = kv.cu[b + 1], len = kv.plens[b];
+        const int t0 = min(max(c0, 0), kv.T - 1), S = min(max(c1 - t0, 1), kv.T - t0), L = min(max(len, 0), kv.max_blocks * 16);
+        const Count4 c = count_items(L, S, G, kv.Hkv, rows_log2, plan.per_log2);
+        const bool in = k + lane < plan.nb;
+        const int n = in ? (MERGE ? c.merge_rows : c.items) : 0, rec = in ? c.records : 0;
+        const int n_sum = scan64(n), rec_sum = scan64(rec);
+        const unsigned long long behind = __ballot((unsigned)(items0 + n_sum) > item);
+        if (behind) {
+            const int l = __builtin_ctzll(behind);
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+            f = Place4{min(plan.b0 + k + l, kv.B - 1), of(t0), of(S), of(L), of(c.pieces), of(c.tiles), (int)item - items0 - of(n_sum - n), records0 + of(rec_sum - rec), true};
+            break;
+        }
+        items0 += __builtin_amdgcn_readlane(n_sum, 63);
+        records0 += __builtin_amdgcn_readlane(rec_sum, 63);
+    }
+    return f;
 }
 
 constexpr int O_PAD = 132;            // floats from row to row of O in LDS
 
 // WR x WK wavefronts: WR take different rows, WK different chunks of keys.
 template <int NQ, int WR, int WK>
-__global__ __launch_bounds__(WR * WK * 64, NQ == 1 ? 3 : 2) void kv4_attn_kernel(Kv4Attn a, AttnPlan4 plan, float *part_o, float2 *part_ml) {
-    constexpr int ROWS = 16 * NQ * WR;
+__global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2 ? 2 : 1) void kv4_attn_kernel(Kv4Attn a, AttnPlan4 plan, float *part_o, float2 *part_ml) {
+    constexpr int ROWS = 16 * NQ * WR, ROWS_LOG2 = __builtin_ctz(ROWS);
+    static_assert((ROWS & (ROWS - 1)) == 0, "");
     __shared__ float s_o[WK > 1 ? WK * ROWS * O_PAD : 1];
     __shared__ float2 s_ml[WK > 1 ? WK * ROWS : 1];
     const Kv4Batch &kv = a.b;
@@ -478,14 +530,11 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 ? 3 : 2) void kv4_attn_kernel
         const unsigned per = gridDim.x / 8, x = item % 8, rest = gridDim.x % 8;
         item = x * per + min(x, rest) + item / 8;
     }
-    const int bi = plan_trace(plan.start, item, lane), trace = min(plan.b0 + bi, kv.B - 1);
     const int G = a.Hq / kv.Hkv;
-    const int t0 = min(max(kv.cu[trace], 0), kv.T - 1), S = min(max(kv.cu[trace + 1] - t0, 1), kv.T - t0);
-    const int L = min(max(kv.plens[trace], 0), kv.max_blocks * 16);
-    const int n_rows = G * S, n_tiles = (n_rows + ROWS - 1) / ROWS, P = plan.pieces[bi];
-    const int local = (int)(item - plan.start[bi]);
-    const int rt = local % n_tiles, piece = local / n_tiles % P, h = local / n_tiles / P;
-    if (h >= kv.Hkv) return;          // (only where device and host lengths differ)
+    const Place4 f = find_item<false>(kv, plan, G, ROWS_LOG2, item, lane);
+    if (!f.found) return;             // (only where device and host lengths differ; so are the record's bounds below)
+    const int trace = f.trace, t0 = f.t0, S = f.S, L = f.L, n_rows = G * S, n_tiles = f.n_tiles, P = f.P;
+    const int rt = f.local % n_tiles, piece = f.local / n_tiles % P, h = f.local / n_tiles / P;
     const int row0 = rt * ROWS + wr * 16 * NQ;
 
     Rows4<NQ> R;
@@ -571,7 +620,8 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 ? 3 : 2) void kv4_attn_kernel
     }
 
     const bool direct = P == 1;
-    const size_t rec = (size_t)plan.part[bi] + ((size_t)(h * n_tiles + rt) * P + piece);
+    const size_t rec = (size_t)f.first_record + ((size_t)(h * n_tiles + rt) * P + piece);
+    if (!direct && rec >= (size_t)plan.n_records) return;
     auto store8 = [&](int row_in_tile, int col, const float (&o)[8], float m, float l, bool first) {
         const int row = rt * ROWS + row_in_tile;
         if (row >= n_rows) return;
@@ -628,18 +678,19 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 ? 3 : 2) void kv4_attn_kernel
 }
 
 // One wavefront per (head, row) of the traces that were cut: a lane has two columns.
-__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 plan, int tile_rows, const float *__restrict__ part_o,
+__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 plan, int rows_log2, const float *__restrict__ part_o,
                                                         const float2 *__restrict__ part_ml) {
     const Kv4Batch &kv = a.b;
     const int lane = threadIdx.x & 63;
     const unsigned at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (at >= (unsigned)plan.n_merge_rows) return;
-    const int bi = plan_trace(plan.mrow, at, lane), trace = min(plan.b0 + bi, kv.B - 1), G = a.Hq / kv.Hkv, P = plan.pieces[bi];
-    const int t0 = min(max(kv.cu[trace], 0), kv.T - 1), S = min(max(kv.cu[trace + 1] - t0, 1), kv.T - t0);
-    const int n_rows = G * S, n_tiles = (n_rows + tile_rows - 1) / tile_rows, local = (int)(at - plan.mrow[bi]), h = local / n_rows, row = local % n_rows;
-    if (h >= kv.Hkv) return;
-    const size_t rec = (size_t)plan.part[bi] + (size_t)(h * n_tiles + row / tile_rows) * P;
-    const size_t first = rec * tile_rows + row % tile_rows;
+    const int G = a.Hq / kv.Hkv;
+    const Place4 f = find_item<true>(kv, plan, G, rows_log2, at, lane);
+    if (!f.found) return;
+    const int t0 = f.t0, n_rows = G * f.S, P = f.P, h = f.local / n_rows, row = f.local % n_rows, tile_rows = 1 << rows_log2;
+    const size_t rec = (size_t)f.first_record + (size_t)(h * f.n_tiles + (row >> rows_log2)) * P;
+    if (rec + P > (size_t)plan.n_records) return;
+    const size_t first = rec * tile_rows + (row & (tile_rows - 1));
     float m = M_NONE;
     for (int p = 0; p < P; ++p) m = fmaxf(m, part_ml[first + (size_t)p * tile_rows].x);
     float l = 0.f, o0 = 0.f, o1 = 0.f;
@@ -657,50 +708,56 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 pla
 struct Launch4 {
     AttnPlan4 plan;
     int nq, wr, wk;
-    size_t records;                   // partial records of tile_rows rows
-    int tile_rows() const { return 16 * nq * wr; }
+    int rows_log2() const { return __builtin_ctz(16 * nq * wr); }
+    size_t record_rows() const { return (size_t)plan.n_records << rows_log2(); }
 };
-constexpr int ATT_SLOTS = 1024;       // items a launch is cut into at least, as far as ATT_MIN_CHUNKS lets it
-constexpr int ATT_MIN_CHUNKS = 32;
+// Pieces are a power of two of chunks, of 32 at least, such that a launch has half this many items or more.  Eight wavefronts: one
+// workgroup fits a CU, and what does not fit at once waits for a whole item (32 traces of 1 to 7 tokens: 24.6 us, in twice as many
+// pieces 31); four: two or three fit, and more items even out (16 traces of 32 to 256 tokens: 150 us, in half as many pieces 178).
+constexpr int att_slots(int wk) { return wk == 8 ? 256 : 2048; }
+constexpr int ATT_MIN_LOG2 = 5;
 
+// Rows of a wavefront and wavefronts that share the keys.  32 rows halve the unpacking for each, 16 make more wavefronts; eight
+// wavefronts finish an item sooner, four leave a batch with many items less to merge.  Measured, us (16 rows x 4, 16 x 8, 32 x 4, 32 x 8):
+// 96 tokens on one context of 4096, 12 heads on 2: 16.1, 14.9, 17.6, 17.0;  32 traces of 1 to 7 tokens: 24.8, 25.4, 27, 24.6;  16 traces of
+// 32 to 256 tokens: 241, -, 150, 180;  48 traces of one token, 40 heads on 8: 102.6, 104.
 void plan_launch(Launch4 &p, const int32_t *h_cu, const int32_t *h_lens, int b0, int nb, int Hq, int Hkv) {
     const int G = Hq / Hkv;
-    int64_t max_rows = 0;
-    for (int b = b0; b < b0 + nb; ++b) max_rows = std::max<int64_t>(max_rows, (int64_t)G * (h_cu[b + 1] - h_cu[b]));
-    if (max_rows <= 16) { p.nq = 1; p.wr = 1; p.wk = 4; }
-    else if (max_rows <= 64) { p.nq = 2; p.wr = 1; p.wk = 4; }
-    else { p.nq = 2; p.wr = 4; p.wk = 1; }
-    const int rows = p.tile_rows();
-    auto tiles = [&](int b) { return ((int64_t)G * (h_cu[b + 1] - h_cu[b]) + rows - 1) / rows; };
-    auto chunks = [&](int b) { return ((int64_t)h_lens[b] + 31) / 32 + ((int64_t)h_cu[b + 1] - h_cu[b] + 31) / 32; };
-    int64_t total = 0;
-    for (int b = b0; b < b0 + nb; ++b) total += Hkv * tiles(b) * chunks(b);
-    const int64_t per = std::max<int64_t>(ATT_MIN_CHUNKS, (total + ATT_SLOTS - 1) / ATT_SLOTS);
-    p.plan.b0 = b0;
-    p.records = 0;
-    int64_t items = 0, mrows = 0;
-    bool many_tiles = false;
-    for (int i = 0; i < ATT_TRACES; ++i) {
-        p.plan.start[i] = (uint32_t)items;
-        p.plan.mrow[i] = (uint32_t)mrows;
-        p.plan.part[i] = (uint32_t)p.records;
-        p.plan.pieces[i] = 1;
-        if (i >= nb) continue;
-        const int b = b0 + i;
-        const int64_t P = std::min<int64_t>((chunks(b) + per - 1) / per, 1024), n = Hkv * tiles(b) * P;
-        p.plan.pieces[i] = (uint16_t)P;
-        many_tiles |= tiles(b) > 1;
-        items += n;
-        if (P > 1) {
-            p.records += n;
-            mrows += (int64_t)Hkv * G * (h_cu[b + 1] - h_cu[b]);
-        }
+    int max_S = 0;
+    int64_t units = 0;                // tiles of 32 rows
+    for (int b = b0; b < b0 + nb; ++b) {
+        const int S = h_cu[b + 1] - h_cu[b];
+        max_S = std::max(max_S, S);
+        units += (int64_t)Hkv * (((int64_t)G * S + 31) / 32);
     }
-    p.plan.start[ATT_TRACES] = (uint32_t)items;
-    p.plan.mrow[ATT_TRACES] = (uint32_t)mrows;
-    p.plan.n_items = (int32_t)items;
-    p.plan.n_merge_rows = (int32_t)mrows;
-    p.plan.swizzle = many_tiles;
+    p.nq = (int64_t)G * max_S <= 16 || units < 64 ? 1 : 2;
+    p.wr = 1;
+    p.wk = units >= 256 ? 4 : 8;
+#ifdef KV4_TUNE
+    if (getenv("KV4_CFG")) sscanf(getenv("KV4_CFG"), "%d,%d,%d", &p.nq, &p.wr, &p.wk);
+    const int64_t slots = getenv("KV4_SLOTS") ? atoi(getenv("KV4_SLOTS")) : att_slots(p.wk), ATT_MIN_LOG2 = getenv("KV4_MIN") ? atoi(getenv("KV4_MIN")) : 5;
+#else
+    const int64_t slots = att_slots(p.wk);
+#endif
+    auto add = [&](int per_log2) {
+        AttnPlan4 &a = p.plan;
+        a = AttnPlan4{b0, nb, per_log2, 0, 0, 0, 0};
+        for (int b = b0; b < b0 + nb; ++b) {
+            const Count4 c = count_items(h_lens[b], h_cu[b + 1] - h_cu[b], G, Hkv, p.rows_log2(), per_log2);
+            a.n_items += c.items;
+            a.n_records += c.records;
+            a.n_merge_rows += c.merge_rows;
+            a.swizzle |= c.tiles > 1;
+        }
+    };
+    int64_t total = 0;                // chunks of all tiles
+    for (int b = b0; b < b0 + nb; ++b) {
+        const int S = h_cu[b + 1] - h_cu[b];
+        total += (int64_t)Hkv * count_items(0, S, G, Hkv, p.rows_log2(), 26).tiles * (((int64_t)h_lens[b] + 31) / 32 + (S + 31) / 32);
+    }
+    int per_log2 = ATT_MIN_LOG2;
+    while (per_log2 < 26 && total > slots << per_log2) ++per_log2;
+    add(per_log2);
 }
 
 }  // namespace
@@ -719,8 +776,8 @@ hipError_t launch_kv4_read(const Kv4Batch &b, float *k, float *v, hipStream_t s)
 }
 
 namespace {
-size_t part_o_bytes(const Launch4 &p) { return p.records * p.tile_rows() * 128 * sizeof(float); }
-size_t part_ml_bytes(const Launch4 &p) { return p.records * p.tile_rows() * sizeof(float2); }
+size_t part_o_bytes(const Launch4 &p) { return p.record_rows() * 128 * sizeof(float); }
+size_t part_ml_bytes(const Launch4 &p) { return p.record_rows() * sizeof(float2); }
 }  // namespace
 
 size_t kv4_attn_scratch(const int32_t *h_cu, const int32_t *h_lens, int B, int Hq, int Hkv) {
@@ -740,12 +797,17 @@ hipError_t launch_kv4_attn(const Kv4Attn &a, const int32_t *h_cu, const int32_t 
         float *part_o = (float *)scratch;
         float2 *part_ml = (float2 *)((char *)scratch + part_o_bytes(p));
         const int threads = 64 * p.wr * p.wk;
-        if (p.nq == 1) kv4_attn_kernel<1, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        else if (p.wr == 1) kv4_attn_kernel<2, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        else kv4_attn_kernel<2, 4, 1><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+#ifdef KV4_TUNE
+#define TRY(A, B, C) else if (p.nq == A && p.wr == B && p.wk == C) kv4_attn_kernel<A, B, C><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        if (0) {} TRY(1, 1, 2) TRY(2, 2, 2) TRY(2, 4, 1) TRY(2, 2, 4) TRY(4, 1, 4) else
+#endif
+        if (p.nq == 2 && p.wk == 8) kv4_attn_kernel<2, 1, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else if (p.nq == 2) kv4_attn_kernel<2, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else if (p.wk == 4) kv4_attn_kernel<1, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else kv4_attn_kernel<1, 1, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
         if (hipError_t e = hipGetLastError()) return e;
         if (p.plan.n_merge_rows) {
-            kv4_merge_kernel<<<(p.plan.n_merge_rows + 3) / 4, 256, 0, s>>>(a, p.plan, p.tile_rows(), part_o, part_ml);
+            kv4_merge_kernel<<<(p.plan.n_merge_rows + 3) / 4, 256, 0, s>>>(a, p.plan, p.rows_log2(), part_o, part_ml);
             if (hipError_t e = hipGetLastError()) return e;
         }
     }
