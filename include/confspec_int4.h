@@ -54,7 +54,8 @@ typedef struct {
  *                  qkv_stride >= (Hq + 2 Hkv) * 128 elements, a multiple of 4
  *   dev_n_append / h_n_append : int32 [B] on the device and on the host (same values), 0 <= n_append[b] <= S_b;
  *                  both NULL: all tokens
- * The rows written must lie inside the block table's capacity, and no two traces may write the same row. */
+ * The rows written must lie inside the block table's capacity, positions below 2^31 - 2^23, and no two traces may write the same
+ * row. */
 int confspec_op_kv4_append(confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_batch *batch, int32_t layer,
                            const float *dev_qkv, int64_t qkv_stride, const int32_t *dev_n_append, const int32_t *h_n_append,
                            void *dev_q, void *dev_k, void *dev_v, confspec_stream stream);
@@ -79,7 +80,7 @@ int confspec_op_kv4_attention_scratch_bytes(const confspec_ctx *ctx, const confs
 
 /* ---- products with 4-bit weights ----
  * A weight is s * (c - z): codes c in 0..15 and, for every row and every group of 32, 64 or 128 elements along k, two
- * IEEE halves s and z (z in units of the code, 8 where it is not given). */
+ * IEEE halves s and z (z in units of the code and kept to 2^-21 of one; 8 where it is not given). */
 #define CONFSPEC_W4_MAX_ROWS 128
 
 /* Bytes confspec_w4_pack writes for an [N, K] matrix; 0 where the shape is not supported (N % 16 != 0, group not 32, 64

@@ -1317,6 +1317,14 @@ int check_int4_ctx(const confspec_ctx *ctx) {
 }
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
+int check_positions(const confspec_ctx *ctx, const confspec_batch *batch) {
+    for (int b = 0; b < batch->B; ++b) {
+        const int64_t end = (int64_t)batch->h_prefix_lens[b] + batch->h_cu_suffix[b + 1] - batch->h_cu_suffix[b];
+        if (end > cs::KV4_MAX_POS) return fail(ctx, CONFSPEC_E_OUT_OF_RANGE, "trace %d ends at position %lld", b, (long long)end);
+    }
+    return CONFSPEC_OK;
+}
+
 // Checks cache, layer and batch; rows (may be null: the context alone has to fit) = rows behind each context that are touched.
 int check_kv4(const confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_batch *batch, int32_t layer, bool touch_suffix,
               const int32_t *h_rows, cs::Kv4Batch *out) {
@@ -1330,11 +1338,9 @@ int check_kv4(const confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_ba
     if (!aligned16(kv->pages)) return fail(ctx, CONFSPEC_E_INVALID_ARG, "kv pages must be 16-byte aligned");
     if (layer < 0 || layer >= (c.n_layers > 0 ? c.n_layers : 1)) return fail(ctx, CONFSPEC_E_INVALID_ARG, "layer %d out of range", layer);
     const int64_t cap = (int64_t)kv->max_blocks_per_seq * 16;
-    if ((rc = check_batch(ctx, batch, cap, nullptr))) return rc;
-    for (int b = 0; b < batch->B; ++b) {
+    if ((rc = check_batch(ctx, batch, cap, nullptr)) || (rc = check_positions(ctx, batch))) return rc;
+    for (int b = 0; touch_suffix && b < batch->B; ++b) {
         const int S = batch->h_cu_suffix[b + 1] - batch->h_cu_suffix[b], L = batch->h_prefix_lens[b];
-        if ((int64_t)L + S > INT32_MAX - 4096) return fail(ctx, CONFSPEC_E_OUT_OF_RANGE, "trace %d ends at position %lld", b, (long long)L + S);
-        if (!touch_suffix) continue;
         const int n = h_rows ? h_rows[b] : S;
         if (n < 0 || n > S) return fail(ctx, CONFSPEC_E_OUT_OF_RANGE, "n_append[%d] = %d outside [0, S_b = %d]", b, n, S);
         if ((int64_t)L + n > cap)
@@ -1342,7 +1348,7 @@ int check_kv4(const confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_ba
     }
     *out = cs::Kv4Batch{batch->cu_suffix, batch->prefix_lens, kv->block_table,
                         (uint8_t *)kv->pages + (size_t)layer * kv->n_blocks * c.n_kv_heads * cs::KV4_PAGE,
-                        batch->B, batch->T, c.n_kv_heads, kv->n_blocks, kv->max_blocks_per_seq};
+                        batch->B, batch->T, c.n_kv_heads, kv->n_blocks, kv->max_blocks_per_seq, (int32_t)std::min<int64_t>(cap, cs::KV4_MAX_POS)};
     return CONFSPEC_OK;
 }
 }  // namespace
@@ -1389,7 +1395,7 @@ int confspec_op_kv4_read(confspec_ctx *ctx, const confspec_kv4 *kv, const confsp
 int confspec_op_kv4_attention_scratch_bytes(const confspec_ctx *ctx, const confspec_batch *batch, size_t *out_bytes) {
     if (!ctx || !out_bytes) return CONFSPEC_E_INVALID_ARG;
     int rc;
-    if ((rc = check_int4_ctx(ctx)) || (rc = check_batch(ctx, batch, INT32_MAX, nullptr))) return rc;
+    if ((rc = check_int4_ctx(ctx)) || (rc = check_batch(ctx, batch, INT32_MAX, nullptr)) || (rc = check_positions(ctx, batch))) return rc;
     *out_bytes = cs::kv4_attn_scratch(batch->h_cu_suffix, batch->h_prefix_lens, batch->B, ctx->cfg.n_q_heads, ctx->cfg.n_kv_heads);
     return CONFSPEC_OK;
 }

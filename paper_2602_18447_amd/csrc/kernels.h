@@ -332,7 +332,9 @@ struct Kv4Batch {
     const int32_t *cu, *plens, *table;
     uint8_t *pages;           // this layer's pages [n_blocks, Hkv, KV4_PAGE]
     int32_t B, T, Hkv, n_blocks, max_blocks;
+    int32_t max_L;            // context lengths are at most this (the table's rows, KV4_MAX_POS)
 };
+constexpr int32_t KV4_MAX_POS = INT32_MAX - (1 << 23);      // positions: sums with a suffix or a chunk stay in 31 bits
 struct Kv4Append {
     Kv4Batch b;
     const float *qkv;

@@ -77,8 +77,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
     const float *src = a.qkv + (size_t)t * a.stride + 2 * i2;
     float2 lo = *(const float2 *)(src + (size_t)min(h, heads - 1) * 128), hi = *(const float2 *)(src + (size_t)min(h, heads - 1) * 128 + 64);
     const int trace = trace_of(b.cu, b.B, t, lane);
-    const int i = min(max(t - b.cu[trace], 0), b.T - 1), L = max(b.plens[trace], 0), row = L + i, slot = row & 15;
-    const bool store = (!a.n_append || i < a.n_append[trace]) && row >= 0 && row < b.max_blocks * 16;
+    const int i = min(max(t - b.cu[trace], 0), b.T - 1), row = min(max(b.plens[trace], 0), b.max_L) + i, slot = row & 15;
+    const bool store = (!a.n_append || i < a.n_append[trace]) && row >> 4 < b.max_blocks;
     uint8_t *const pages = page_of(b, trace, row, 0);
     // theta^(-j / 64) for j = 2 i and 2 i + 1, from its six powers of two (64 values in the arguments would be 2 us away, in host memory)
     double f0 = i2 & 1 ? a.theta_pow[1] : 1.0;
@@ -144,7 +144,7 @@ __device__ __forceinline__ float param_z(unsigned p) { return __half2float(__ush
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, float *__restrict__ k, float *__restrict__ v) {
     const int t = blockIdx.x / n_split, h = blockIdx.x % n_split * 8 + (threadIdx.x >> 5);
     const int trace = trace_of(b.cu, b.B, t, threadIdx.x & 63);
-    const int row = max(b.plens[trace], 0) + min(max(t - b.cu[trace], 0), b.T - 1), slot = row & 15;
+    const int row = min(max(b.plens[trace], 0), b.max_L) + min(max(t - b.cu[trace], 0), b.T - 1), slot = row & 15;
     if (h >= b.Hkv) return;
     const int is_v = (threadIdx.x >> 4) & 1, d = (threadIdx.x & 15) * 8;
     const uint8_t *page = page_of(b, trace, row, h);
@@ -495,7 +495,7 @@ __device__ __forceinline__ Place4 find_item(const Kv4Batch &kv, const AttnPlan4 
     for (int k = 0; k < plan.nb; k += 64) {
         const int b = min(plan.b0 + min(k + lane, plan.nb - 1), kv.B - 1);
         const int c0 = kv.cu[b], c1 = kv.cu[b + 1], len = kv.plens[b];
-        const int t0 = min(max(c0, 0), kv.T - 1), S = min(max(c1 - t0, 1), kv.T - t0), L = min(max(len, 0), kv.max_blocks * 16);
+        const int t0 = min(max(c0, 0), kv.T - 1), S = min(max(c1 - t0, 1), kv.T - t0), L = min(max(len, 0), kv.max_L);
         const Count4 c = count_items(L, S, G, kv.Hkv, rows_log2, plan.per_log2);
         const bool in = k + lane < plan.nb;
         const int n = in ? (MERGE ? c.merge_rows : c.items) : 0, rec = in ? c.records : 0;
@@ -691,15 +691,38 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 pla
     const size_t rec = (size_t)f.first_record + (size_t)(h * f.n_tiles + (row >> rows_log2)) * P;
     if (rec + P > (size_t)plan.n_records) return;
     const size_t first = rec * tile_rows + (row & (tile_rows - 1));
-    float m = M_NONE;
-    for (int p = 0; p < P; ++p) m = fmaxf(m, part_ml[first + (size_t)p * tile_rows].x);
-    float l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int p = 0; p < P; ++p) {
-        const float2 ml = part_ml[first + (size_t)p * tile_rows], o = *(const float2 *)(part_o + (first + (size_t)p * tile_rows) * 128 + 2 * lane);
-        const float f = __builtin_amdgcn_exp2f(ml.x - m);
-        l += f * ml.y;
-        o0 += f * o.x;
-        o1 += f * o.y;
+    const float *o = part_o + first * 128 + 2 * lane;
+    const size_t step = (size_t)tile_rows * 128;
+    // 64 pieces a round: a lane has the maximum and sum of one, and all their rows of O are asked for before they are needed
+    float m = M_NONE, l = 0.f, o0 = 0.f, o1 = 0.f;
+    for (int p0 = 0; p0 < P; p0 += 64) {
+        const int n = min(64, P - p0);
+        const float2 ml = lane < n ? part_ml[first + (size_t)(p0 + lane) * tile_rows] : make_float2(M_NONE, 0.f);
+        float top = ml.x;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+        top = fmaxf(top, m);
+        const float keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+        float sum = f * ml.y;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+        m = top;
+        l = l * keep + sum;
+        o0 *= keep;
+        o1 *= keep;
+        for (int p = 0; p < n; p += 4) {
+            float2 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = p + u < n ? *(const float2 *)(o + (size_t)(p0 + p + u) * step) : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), min(p + u, n - 1)));
+                if (p + u < n) {
+                    o0 += w * v[u].x;
+                    o1 += w * v[u].y;
+                }
+            }
+        }
     }
     *(unsigned *)(a.out + ((size_t)(t0 + row / G) * a.Hq + h * G + row % G) * 128 + 2 * lane) = pack_bf16(o0 / l, o1 / l);
 }

@@ -116,6 +116,7 @@ def test_cache_operators_refuse_bad_arguments():
     far.kv.max_blocks_per_seq = 2 ** 27
     for call in (far.append, far.read, far.attn):
         _refused(cb.E_OUT_OF_RANGE, call)
+    _refused(cb.E_OUT_OF_RANGE, cb.confspec_op_kv4_attention_scratch_bytes, far.ctx, far.batch)
     f32 = _Args("fp32")
     for call in (f32.append, f32.read, f32.attn):
         _refused(cb.E_UNSUPPORTED, call)
@@ -167,3 +168,19 @@ def test_weight_sizes_and_refusals():
     cb.confspec_destroy(ctx)
     cb.confspec_destroy(f32)
     assert cb.lib.confspec_op_w4_gemm(None, None, None, None, None, 1, 16, 32, 32, 0, None) == cb.E_INVALID_ARG
+
+
+@pytest.mark.parametrize("Hq, Hkv", [(12, 2), (40, 8), (64, 64), (128, 1)])
+def test_attention_scratch_stays_small(Hq, Hkv):
+    """Partial results are kept for at most about twice 2048 pieces of 32 rows, whatever the batch."""
+    ctx = cb.confspec_create(_cfg(n_q_heads=Hq, n_kv_heads=Hkv))
+    rng = np.random.default_rng(Hq)
+    for _ in range(300):
+        B = int(rng.choice([1, 2, 30, 256, 257, 900]))
+        L = rng.integers(0, int(rng.choice([1, 100, 5000, 1 << 20, 1 << 30])) + 1, B).astype(np.int32)
+        S = rng.integers(1, int(rng.choice([1, 8, 300, 4000])) + 1, B)
+        cu = np.concatenate([[0], np.cumsum(S)]).astype(np.int32)
+        d = _FakeDev()
+        batch, keep = cb.make_batch(d, d, d, cu, L)
+        assert cb.confspec_op_kv4_attention_scratch_bytes(ctx, batch) <= 2 * 2049 * 32 * 130 * 4, (B, L.max(), S.max())
+    cb.confspec_destroy(ctx)
