@@ -164,13 +164,14 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, 
 // chunks of 32 tokens: two pages of the cache, then 32 tokens of the suffix at a time.  It shares nothing with other
 // wavefronts until the end and keeps its own (maximum, sum, O).
 //  * Scores S^T = K Q^T: a page's key codes are the first operand of four 16x16x32 products as they lie in memory, 16
-//    bytes a lane; code c enters as the bfloat16 16 + c (the code's four bits put into the mantissa of 16), which is
-//    exact, and the sum starts at -16 sum(q), so that it ends as sum q c.  A lane then has four keys of one query row:
-//    score = s sum + z sum(q), two multiply-adds that take s and z as the halves they are.
+//    bytes a lane.  A code enters as a half below the normal range, its four bits alone: c 2^-24, or c 2^-20 where they stay in the
+//    next four bits, and such elements of q are 1/16 of what they are: two of four codes need no shift.  q is a half too, times a
+//    power of two of its row that brings its largest element to 2^13 .. 2^14: exact but for elements 2^-27 times smaller.  A lane then has
+//    four keys of one query row: score = s sum + z sum(q), two multiply-adds that take s and z as the halves they are.
 //  * O^T = V^T P^T: the lane's four keys of both pages are the eight consecutive k of the second operand as they are, and
-//    a page's value codes lie in memory such that a lane's 16 bytes are those four tokens of eight columns.  Code c
-//    enters as the half c 2^-24 (its four bits alone), the probability as the half p s; z is added to the row's sum.
-//    The lane has 32 columns of its one query row, so scaling, sums and output need nothing of other lanes.
+//    a page's value codes lie in memory such that a lane's 16 bytes are those four tokens of eight columns.  Codes enter as
+//    the keys' do, the probability as the half p s; z is added to the row's sum.  The lane has 32 columns of its one query row,
+//    so scaling, sums and output need nothing of other lanes.
 //  * The running reference M of a row is a bound of score + exponent of s (p s is what must fit a half); it is raised,
 //    and what was summed scaled, only where a row goes beyond it by more than 2^8.
 //
@@ -194,18 +195,10 @@ __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __bui
 __device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ unsigned lo_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }   // b.lo : a.lo
 __device__ __forceinline__ unsigned hi_halves(unsigned a, unsigned b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-// Eight key codes as bfloat16 16 + c: element 2 k and 2 k + 1 are nibbles k and k + 4.
-struct CodeBits { unsigned mask, one; };   // in registers: one and-or takes both only if neither is a literal
-__device__ __forceinline__ CodeBits code_bits() {
-    CodeBits b;
-    asm("s_mov_b32 %0, 0x780078" : "=s"(b.mask));
-    asm("v_mov_b32 %0, 0x41804180" : "=v"(b.one));
-    return b;
-}
-__device__ __forceinline__ bf16x8 key_codes(unsigned w, CodeBits b) {
-    const unsigned M = b.mask, C = b.one;
-    const u32x4 r = {((w << 3) & M) | C, ((w >> 1) & M) | C, ((w >> 5) & M) | C, ((w >> 9) & M) | C};
-    return __builtin_bit_cast(bf16x8, r);
+// Four pairs of codes as halves: nibbles 0 and 2 of each 16 bits times 2^-24, nibbles 1 and 3 times 2^-20.
+__device__ __forceinline__ u32x4 code_halves(unsigned w) {
+    const unsigned u = w >> 8;
+    return u32x4{w & 0x000F000Fu, w & 0x00F000F0u, u & 0x000F000Fu, u & 0x00F000F0u};
 }
 __device__ __forceinline__ unsigned pack_f16(float a, float b) {
     const f32x2 v = {a, b};
@@ -227,8 +220,12 @@ __device__ __forceinline__ float sum_over_g(float v) {
 constexpr float SCALE_LOG2 = 0.08838834764831845f * 1.4426950408889634f;
 // References: M bounds score + exponent field of s (15 where s is 1), all in powers of two; p = 2^(score - M + REF).
 // Then p s < 2^(M_ROOM + 6) = 2^14 whatever the rows' s are, and a half ends at 2^16; p itself stays below 2^(M_ROOM + REF).
-constexpr float M_NONE = -1e30f, M_ROOM = 8.f, REF = 20.f, E_ONE = 15.f;
-constexpr float V_UNIT = 1.f / 16777216.f;
+constexpr float M_NONE = -3e38f, M_ROOM = 8.f, REF = 20.f, E_ONE = 15.f;
+// Scores beyond this are rounded before the reference is taken off: below, a multiply-add does both, whose unrounded product differs
+// from what the reference was rounded from by less than 2^-10.
+constexpr float BIG = 16384.f;
+// Sums of the value product are in units of 2^-24 in even and of 2^-20 in odd columns.
+constexpr float UNIT_EVEN = 1.f / 16777216.f, UNIT_ODD = 1.f / 1048576.f;
 
 // Loads of 16 bytes from a wave-uniform base plus a byte offset per lane; offsets at or past the end read zeros.
 struct Loads {
@@ -244,19 +241,15 @@ struct Chunk4 {
 
 template <int NQ>
 struct Rows4 {                        // state of a wavefront's rows: a lane has row lane % 16 of each 16
-    bf16x8 q[NQ][4];
-    f32x4 q_off[NQ];                  // -16 sum(q), four times
-    float q_sum[NQ], m[NQ], l[NQ], zs[NQ];
-    f32x4 o[NQ][8];                   // [j][r]: column 32 (lane / 16) + 8 r + j, in units of 2^-24
+    f16x8 q[NQ][4];                   // times a power of two of the row; elements 2, 3, 6, 7 of eight 1/16 of it
+    float scale[NQ];                  // log2(e) / sqrt(128), that power and the codes' 2^-24 taken out
+    float q_sum[NQ], m[NQ], l[NQ], zs[NQ];      // q_sum: sum(q) in the units of the product
+    f32x4 o[NQ][8];                   // [j][r]: column 32 (lane / 16) + 8 r + j
 };
 
-// Raises the references where needed; t_max: the lane's largest score + exponent.
+// Raises the references to the rows' largest score + exponent (t_max: the lane's).
 template <int NQ>
 __device__ __forceinline__ void raise(Rows4<NQ> &R, const float (&t_max)[NQ]) {
-    bool over = false;
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) over |= t_max[i] > R.m[i] + M_ROOM;
-    if (!__any(over)) return;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
         const float m = fmaxf(R.m[i], max_over_g(t_max[i])), f = __builtin_amdgcn_exp2f(R.m[i] - m);
@@ -273,15 +266,15 @@ __device__ __forceinline__ float mix_z(unsigned p, float a, float b) { return fm
 
 // 32 cached tokens, of which the first n_valid count; what is stored for the others may be anything.
 template <int NQ>
-__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g, CodeBits bits) {
+__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g) {
     f32x4 sc[NQ][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const bf16x8 a = key_codes(c.k[x][i], bits);
+            const f16x8 a = __builtin_bit_cast(f16x8, code_halves(c.k[x][i]));
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) sc[n][x] = mma(a, R.q[n][i], i == 0 ? R.q_off[n] : sc[n][x]);
+            for (int n = 0; n < NQ; ++n) sc[n][x] = mma(a, R.q[n][i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[n][x]);
         }
     u32x4 vp[2] = {c.vp[0], c.vp[1]};
 #pragma unroll
@@ -309,23 +302,58 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
         for (int r = 0; r < 4; ++r) {
             const float e = (float)((vp[x][r] >> 10) & 31u);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) t_max[n] = fmaxf(t_max[n], fmaf(sc[n][x][r], SCALE_LOG2, e));
+            for (int n = 0; n < NQ; ++n) t_max[n] = fmaxf(t_max[n], fmaf(sc[n][x][r], R.scale[n], e));
         }
-    raise<NQ>(R, t_max);
+    bool over = false, big = false;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) big |= fabsf(t_max[n]) > BIG && fabsf(t_max[n]) < INFINITY;
+    big = __any(big);
+    if (big) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            t_max[n] = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sc[n][x][r] *= R.scale[n];
+                    t_max[n] = fmaxf(t_max[n], sc[n][x][r] + (float)((vp[x][r] >> 10) & 31u));
+                }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) over |= t_max[n] > R.m[n] + M_ROOM;
+    if (__any(over)) raise<NQ>(R, t_max);
+    if (big) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)   // (an exponent added to such a score may be lost: p s is bounded by itself)
+                    sc[n][x][r] = fminf((sc[n][x][r] - R.m[n]) + REF, M_ROOM + REF - (float)((vp[x][r] >> 10) & 31u));
+    } else {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const float ref = REF - R.m[n];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sc[n][x][r] = fmaf(sc[n][x][r], R.scale[n], ref);
+        }
+    }
     f16x8 w[NQ];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const float ref = REF - R.m[n];
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(sc[n][x][r], SCALE_LOG2, ref));
+                const float p = __builtin_amdgcn_exp2f(sc[n][x][r]);
                 R.l[n] += p;
                 R.zs[n] = mix_z(vp[x][r], p, R.zs[n]);
                 w[n][4 * x + r] = (_Float16)mix(vp[x][r], p, 0.f);
             }
-    }
     unsigned lo[4], hi[4];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -335,12 +363,18 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
             hi[2 * x + r] = hi_halves(c.v[x][2 * r], c.v[x][2 * r + 1]);
         }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        u32x4 a;
+    for (int h = 0; h < 2; ++h) {
+        u32x4 col[4];                 // columns 4 h .. 4 h + 3
 #pragma unroll
-        for (int r = 0; r < 4; ++r) a[r] = ((j < 4 ? lo[r] : hi[r]) >> (4 * (j & 3))) & 0x000F000Fu;
+        for (int r = 0; r < 4; ++r) {
+            const u32x4 v = code_halves(h ? hi[r] : lo[r]);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) R.o[n][j] = mma(__builtin_bit_cast(f16x8, a), w[n], R.o[n][j]);
+            for (int j = 0; j < 4; ++j) col[j][r] = v[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) R.o[n][4 * h + j] = mma(__builtin_bit_cast(f16x8, col[j]), w[n], R.o[n][4 * h + j]);
     }
 }
 
@@ -348,8 +382,13 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
 // sees tokens up to its own (tok).  Products in bfloat16, probabilities in two terms.  True: values were taken out that
 // add_not_finite has to add.
 template <int NQ>
-__device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *k, const bf16 *v, size_t stride, int j0, int S, const int (&tok)[NQ],
-                                             int n15, int g) {
+__device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *q, const int (&q_row)[NQ], const bf16 *k, const bf16 *v, size_t stride, int j0,
+                                             int S, const int (&tok)[NQ], int n15, int g) {
+    bf16x8 qb[NQ][4];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qb[n][i] = *(const bf16x8 *)(q + (size_t)q_row[n] * 128 + 8 * g + 32 * i);
     f32x4 sc[NQ][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -358,7 +397,7 @@ __device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *k, const 
         for (int i = 0; i < 4; ++i) {
             const bf16x8 a = *(const bf16x8 *)(row + 32 * i);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) sc[n][x] = mma(a, R.q[n][i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[n][x]);
+            for (int n = 0; n < NQ; ++n) sc[n][x] = mma(a, qb[n][i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[n][x]);
         }
     }
     u32x4 vw[8];
@@ -402,25 +441,27 @@ __device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *k, const 
                     if ((vw[t][e] & 0x7f800000u) == 0x7f800000u) vw[t][e] &= 0xffffu;
                 }
     }
-    raise<NQ>(R, t_max);
-    u32x4 hi[NQ], lo[NQ];
+    bool over = false;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) over |= t_max[n] > R.m[n] + M_ROOM;
+    if (__any(over)) raise<NQ>(R, t_max);
+    u32x4 hi[NQ][2], lo[NQ][2];       // in the units of even and of odd columns
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        const float ref = REF - R.m[n];
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 4; r += 2) {
-                float p0 = __builtin_amdgcn_exp2f(sc[n][x][r] + ref), p1 = __builtin_amdgcn_exp2f(sc[n][x][r + 1] + ref);
+                const float p0 = __builtin_amdgcn_exp2f((sc[n][x][r] - R.m[n]) + REF), p1 = __builtin_amdgcn_exp2f((sc[n][x][r + 1] - R.m[n]) + REF);
                 R.l[n] += p0;
                 R.l[n] += p1;
-                p0 *= V_UNIT;
-                p1 *= V_UNIT;
-                sc[n][x][r] = p0;
-                sc[n][x][r + 1] = p1;
-                const unsigned h = pack_bf16(p0, p1);
-                hi[n][2 * x + (r >> 1)] = h;
-                lo[n][2 * x + (r >> 1)] = pack_bf16(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float a0 = p0 * (u ? UNIT_ODD : UNIT_EVEN), a1 = p1 * (u ? UNIT_ODD : UNIT_EVEN);
+                    const unsigned h = pack_bf16(a0, a1);
+                    hi[n][u][2 * x + (r >> 1)] = h;
+                    lo[n][u][2 * x + (r >> 1)] = pack_bf16(a0 - __uint_as_float(h << 16), a1 - __uint_as_float(h & 0xffff0000u));
+                }
             }
     }
 #pragma unroll
@@ -432,8 +473,8 @@ __device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *k, const 
         const bf16x8 av = __builtin_bit_cast(bf16x8, a);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, hi[n]), R.o[n][j]);
-            R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, lo[n]), R.o[n][j]);
+            R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, hi[n][j & 1]), R.o[n][j]);
+            R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, lo[n][j & 1]), R.o[n][j]);
         }
     }
     return bad;
@@ -538,21 +579,34 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2
     const int row0 = rt * ROWS + wr * 16 * NQ;
 
     Rows4<NQ> R;
-    int tok[NQ];
+    int tok[NQ], q_row[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const int row = min(row0 + 16 * n + n15, n_rows - 1);
         tok[n] = row / G;
-        const bf16 *q = a.q + ((size_t)(t0 + tok[n]) * a.Hq + h * G + row % G) * 128 + 8 * g;
-        float sum = 0.f;
+        q_row[n] = (t0 + tok[n]) * a.Hq + h * G + row % G;
+        const bf16 *q = a.q + (size_t)q_row[n] * 128 + 8 * g;
+        bf16x8 v[4];
+        float sum = 0.f, top = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            R.q[n][i] = *(const bf16x8 *)(q + 32 * i);
+            v[i] = *(const bf16x8 *)(q + 32 * i);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += (float)R.q[n][i][e];
+            for (int e = 0; e < 8; ++e) {
+                sum += (float)v[i][e];
+                top = fmaxf(top, fabsf((float)v[i][e]));
+            }
         }
-        R.q_sum[n] = sum_over_g(sum);
-        R.q_off[n] = f32x4{1.f, 1.f, 1.f, 1.f} * (-16.f * R.q_sum[n]);
+        // 2^(14 - x), where x is the exponent behind the row's largest element: between 2^114 and 2^-102
+        const int x = min(max((int)(__float_as_uint(max_over_g(top)) >> 23) - 126, -100), 116);
+        const float up = __uint_as_float((unsigned)(14 - x + 127) << 23);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) R.q[n][i][e] = (_Float16)((float)v[i][e] * (e & 2 ? up * 0.0625f : up));
+        const float unit = __uint_as_float((unsigned)(x + 10 + 127) << 23);      // 2^24 / 2^(14 - x)
+        R.scale[n] = SCALE_LOG2 * unit;
+        R.q_sum[n] = sum_over_g(sum) * __uint_as_float((unsigned)(127 - x - 10) << 23);
         R.m[n] = M_NONE;
         R.l[n] = R.zs[n] = 0.f;
 #pragma unroll
@@ -568,7 +622,6 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2
         const uint8_t *head = kv.pages + (size_t)h * KV4_PAGE;
         const size_t block_bytes = (size_t)kv.Hkv * KV4_PAGE;
         const unsigned at16 = lane * 16, at_kp = KV4_KP + g * 16;
-        const CodeBits bits = code_bits();
         // Block numbers of 32 chunks, two lanes each, and of the 32 after them; chunk i of this wavefront is c_begin + wk + i WK.
         auto block_ids = [&](int i0) {
             const int page = 2 * (c_begin + wk + WK * (i0 + (lane >> 1))) + (lane & 1);
@@ -589,7 +642,7 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2
             __builtin_amdgcn_sched_barrier(0);   // (loads stay ahead of the products before them in time)
         };
         auto compute = [&](const Chunk4 &d, int i) {
-            cached_chunk<NQ>(R, d, L - 32 * (c_begin + wk + WK * i), g, bits);
+            cached_chunk<NQ>(R, d, L - 32 * (c_begin + wk + WK * i), g);
             __builtin_amdgcn_sched_barrier(0);
         };
         const int n = (c_stop - c_begin - wk + WK - 1) / WK;
@@ -614,7 +667,7 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2
         const int my_hi = (min(row0 + 16 * NQ, n_rows) - 1) / G;      // (negative rows cannot be: row0 may lie behind the last row)
         for (; c < c_end; c += WK) {
             const int j0 = 32 * (c - n_cached);
-            if (j0 > my_hi || !suffix_chunk<NQ>(R, k, v, stride, j0, S, tok, n15, g)) continue;
+            if (j0 > my_hi || !suffix_chunk<NQ>(R, a.q, q_row, k, v, stride, j0, S, tok, n15, g)) continue;
             add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
         }
     }
@@ -644,7 +697,7 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2
         for (int r = 0; r < 4; ++r) {
             float o[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = fmaf(R.o[n][j][r], 1.f / V_UNIT, zs);
+            for (int j = 0; j < 8; ++j) o[j] = fmaf(R.o[n][j][r], 1.f / (j & 1 ? UNIT_ODD : UNIT_EVEN), zs);
             if constexpr (WK == 1) {
                 store8(row, 32 * g + 8 * r, o, R.m[n], l, g == 0 && r == 0);
             } else {

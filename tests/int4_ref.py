@@ -84,9 +84,10 @@ def attention(pages, table, q, k, v, cu, lens, Hq, Hkv):
     Terms of the bound, beside half a bf16 step of the result (2^-8 |o|):
       - probabilities times s are halves: half a step, 2^-11, of p_j s_j c_j; suffix probabilities have two bf16
         terms, 2^-16;
-      - scores are fp32: q (16 + c) sums over 128 products exact each, so an error of 136 2^-24 sum |q| (16 + 15 + 24) s
-        and two roundings of s acc + z' sum q, which moves a probability by that times log(e) = the same relative to it;
-        twice, for numerator and denominator; exp2 and the shift cost 2^-20 of p (scores up to 2^6) more;
+      - scores are fp32: q c is a sum of 128 products, each exact (elements of q 2^-27 times the row's largest lose what is below 2^-38
+        of it), so an error of 136 2^-24 sum |q| 15 s and two roundings of s acc + z sum q, which moves a probability by that times
+        log(e) = the same relative to it; twice, for numerator and denominator; exp2 and the shift cost 2^-20 of p (scores up to
+        2^6) more;
       - sums over n keys: added in steps of 32, wavefronts and pieces apart: (n / 32 + 64) 2^-24 of the absolute sum,
         in which s c and z count apart."""
     T, G = q.shape[0], Hq // Hkv
@@ -114,7 +115,7 @@ def attention(pages, table, q, k, v, cu, lens, Hq, Hkv):
             Vall = torch.cat((V, Vs))
             o = p @ Vall
             qa = Q.abs().sum(-1, keepdim=True)
-            es = 2.0 ** -24 * qa * torch.cat((138 * (55 * ks + 2 * kz.abs()), 138 * Ks.abs().max(-1).values)) / math.sqrt(HD)
+            es = 2.0 ** -24 * qa * torch.cat((138 * (16 * ks + 2 * kz.abs()), 138 * Ks.abs().max(-1).values)) / math.sqrt(HD)
             es = torch.where(p > 0, es, torch.zeros_like(es))
             reach = torch.cat((V.abs(), Vs.abs()))
             apart = torch.cat((vz.abs()[:, None] + (V - vz[:, None]).abs(), Vs.abs())) if L else reach

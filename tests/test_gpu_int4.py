@@ -311,6 +311,21 @@ def test_attention_from_even_to_single_weights(q_scale):
     _attn_case(4, 2, (700, 33), (3, 1), 12, q_scale=q_scale)
 
 
+def test_attention_queries_of_any_size():
+    """Rows of q from 1e-30 to 1e30, elements of one row 2^20 apart, and a row of zeros: each as if alone."""
+    gen = _gen(42)
+    Hq, Hkv = 8, 2
+    c = Cache(gen, Hkv, (150, 20), (4, 9))
+    q = torch.randn(c.T, Hq, 128, generator=gen, device=DEV)
+    q = q * torch.tensor([1e-30, 1e-3, 1.0, 3.0, 0.0, 30.0, 1e10, 1e30], device=DEV)[:, None]
+    q[:, 2, ::7] *= 2.0 ** -20
+    k = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV).bfloat16()
+    v = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV).bfloat16()
+    with Ctx(Hq, Hkv) as ctx:
+        out = _attn_check(ctx, c, Hq, Hkv, q.bfloat16(), k, v)
+    assert bool(torch.isfinite(out).all())
+
+
 def test_attention_in_another_layer():
     _attn_case(4, 2, (50, 120), (2, 1), 13, layer=2, n_layers=3)
 
