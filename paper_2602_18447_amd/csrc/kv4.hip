@@ -178,7 +178,8 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, 
 // Bound by the cache's bytes when rows are few (136 bytes a token and head), by the vector pipe when they are many.
 constexpr int ATT_TRACES = 256;       // traces of one launch
 struct AttnPlan4 {
-    int32_t b0, nb, per_log2;         // traces; chunks of keys of a piece at most, a power of two
+    int32_t b0, nb;                   // traces
+    uint32_t per, per_inv;            // chunks of keys of a piece at most, 2^32 / per rounded up
     int32_t n_items, n_records, n_merge_rows;
     int32_t swizzle;
 };
@@ -520,10 +521,11 @@ struct Place4 {
     bool found;
 };
 struct Count4 { int tiles, pieces, items, records, merge_rows; };
-__host__ __device__ inline Count4 count_items(int L, int S, int G, int Hkv, int rows_log2, int per_log2) {
+__host__ __device__ inline Count4 count_items(int L, int S, int G, int Hkv, int rows_log2, uint32_t per, uint32_t per_inv) {
     Count4 c;
     c.tiles = (int)(((long)G * S + (1 << rows_log2) - 1) >> rows_log2);
-    c.pieces = (((L + 31) >> 5) + ((S + 31) >> 5) + (1 << per_log2) - 1) >> per_log2;
+    // rounded up (one more than that, in places, where chunks go into the millions: nothing but this function decides it)
+    c.pieces = (int)(((uint64_t)(((L + 31) >> 5) + ((S + 31) >> 5) + per - 1) * per_inv) >> 32);
     c.items = Hkv * c.tiles * c.pieces;
     c.records = c.pieces > 1 ? c.items : 0;
     c.merge_rows = c.pieces > 1 ? Hkv * G * S : 0;
@@ -537,7 +539,7 @@ __device__ __forceinline__ Place4 find_item(const Kv4Batch &kv, const AttnPlan4 
         const int b = min(plan.b0 + min(k + lane, plan.nb - 1), kv.B - 1);
         const int c0 = kv.cu[b], c1 = kv.cu[b + 1], len = kv.plens[b];
         const int t0 = min(max(c0, 0), kv.T - 1), S = min(max(c1 - t0, 1), kv.T - t0), L = min(max(len, 0), kv.max_L);
-        const Count4 c = count_items(L, S, G, kv.Hkv, rows_log2, plan.per_log2);
+        const Count4 c = count_items(L, S, G, kv.Hkv, rows_log2, plan.per, plan.per_inv);
         const bool in = k + lane < plan.nb;
         const int n = in ? (MERGE ? c.merge_rows : c.items) : 0, rec = in ? c.records : 0;
         const int n_sum = scan64(n), rec_sum = scan64(rec);
@@ -787,16 +789,16 @@ struct Launch4 {
     int rows_log2() const { return __builtin_ctz(16 * nq * wr); }
     size_t record_rows() const { return (size_t)plan.n_records << rows_log2(); }
 };
-// Pieces are a power of two of chunks, of 32 at least, such that a launch has half this many items or more.  Eight wavefronts: one
-// workgroup fits a CU, and what does not fit at once waits for a whole item (32 traces of 1 to 7 tokens: 24.6 us, in twice as many
-// pieces 31); four: two or three fit, and more items even out (16 traces of 32 to 256 tokens: 150 us, in half as many pieces 178).
-constexpr int att_slots(int wk) { return wk == 8 ? 256 : 2048; }
-constexpr int ATT_MIN_LOG2 = 5;
+// Pieces are of 32 chunks at least.  With eight wavefronts one workgroup fits a CU, and what does not fit at once waits for a whole item: as
+// few items as there are CUs (one token on 16384 keys, 12 heads on 2: 13.7 us; in pieces of a power of two of chunks, which leave some CUs
+// without, 18).  With four, two or three fit, and more items even out (16 traces of 32 to 256 tokens: 141 us, with 1024 items 147).
+constexpr int ATT_MIN_CHUNKS = 32;
+constexpr int att_slots(int wk) { return wk == 8 ? 256 : 1536; }
 
 // Rows of a wavefront and wavefronts that share the keys.  32 rows halve the unpacking for each, 16 make more wavefronts; eight
 // wavefronts finish an item sooner, four leave a batch with many items less to merge.  Measured, us (16 rows x 4, 16 x 8, 32 x 4, 32 x 8):
-// 96 tokens on one context of 4096, 12 heads on 2: 16.1, 14.9, 17.6, 17.0;  32 traces of 1 to 7 tokens: 24.8, 25.4, 27, 24.6;  16 traces of
-// 32 to 256 tokens: 241, -, 150, 180;  48 traces of one token, 40 heads on 8: 102.6, 104.
+// 96 tokens on one context of 4096, 12 heads on 2: 15.9, 14.7, 16.3, 16.6;  32 traces of 1 to 7 tokens: 21.9, 20.5, 24, 22.6;  16 traces
+// of 32 to 256 tokens: 228, -, 141, 180;  48 traces of one token, 40 heads on 8: 99, 104.
 void plan_launch(Launch4 &p, const int32_t *h_cu, const int32_t *h_lens, int b0, int nb, int Hq, int Hkv) {
     const int G = Hq / Hkv;
     int max_S = 0;
@@ -806,34 +808,33 @@ void plan_launch(Launch4 &p, const int32_t *h_cu, const int32_t *h_lens, int b0,
         max_S = std::max(max_S, S);
         units += (int64_t)Hkv * (((int64_t)G * S + 31) / 32);
     }
-    p.nq = (int64_t)G * max_S <= 16 || units < 64 ? 1 : 2;
+    p.nq = (int64_t)G * max_S <= 16 || units < 128 ? 1 : 2;
     p.wr = 1;
     p.wk = units >= 256 ? 4 : 8;
+    int slots = att_slots(p.wk), least = ATT_MIN_CHUNKS;
 #ifdef KV4_TUNE
     if (getenv("KV4_CFG")) sscanf(getenv("KV4_CFG"), "%d,%d,%d", &p.nq, &p.wr, &p.wk);
-    const int64_t slots = getenv("KV4_SLOTS") ? atoi(getenv("KV4_SLOTS")) : att_slots(p.wk), ATT_MIN_LOG2 = getenv("KV4_MIN") ? atoi(getenv("KV4_MIN")) : 5;
-#else
-    const int64_t slots = att_slots(p.wk);
+    slots = getenv("KV4_SLOTS") ? atoi(getenv("KV4_SLOTS")) : att_slots(p.wk);
+    if (getenv("KV4_MIN")) least = atoi(getenv("KV4_MIN"));
 #endif
-    auto add = [&](int per_log2) {
-        AttnPlan4 &a = p.plan;
-        a = AttnPlan4{b0, nb, per_log2, 0, 0, 0, 0};
+    AttnPlan4 &a = p.plan;
+    int64_t total = 0;                // chunks of all tiles
+    for (int b = b0; b < b0 + nb; ++b) {
+        const int S = h_cu[b + 1] - h_cu[b];
+        total += (int64_t)Hkv * (((int64_t)G * S + (1 << p.rows_log2()) - 1) >> p.rows_log2()) * (((int64_t)h_lens[b] + 31) / 32 + (S + 31) / 32);
+    }
+    for (int64_t per = std::max<int64_t>(least, (total + slots - 1) / slots);; per += per / 8 + 1) {
+        a = AttnPlan4{b0, nb, (uint32_t)std::min<int64_t>(per, 1 << 27), 0, 0, 0, 0, 0};
+        a.per_inv = (uint32_t)(((1ull << 32) + a.per - 1) / a.per);
         for (int b = b0; b < b0 + nb; ++b) {
-            const Count4 c = count_items(h_lens[b], h_cu[b + 1] - h_cu[b], G, Hkv, p.rows_log2(), per_log2);
+            const Count4 c = count_items(h_lens[b], h_cu[b + 1] - h_cu[b], G, Hkv, p.rows_log2(), a.per, a.per_inv);
             a.n_items += c.items;
             a.n_records += c.records;
             a.n_merge_rows += c.merge_rows;
             a.swizzle |= c.tiles > 1;
         }
-    };
-    int64_t total = 0;                // chunks of all tiles
-    for (int b = b0; b < b0 + nb; ++b) {
-        const int S = h_cu[b + 1] - h_cu[b];
-        total += (int64_t)Hkv * count_items(0, S, G, Hkv, p.rows_log2(), 26).tiles * (((int64_t)h_lens[b] + 31) / 32 + (S + 31) / 32);
+        if (p.wk == 4 || a.n_items <= slots || a.n_records == 0) break;
     }
-    int per_log2 = ATT_MIN_LOG2;
-    while (per_log2 < 26 && total > slots << per_log2) ++per_log2;
-    add(per_log2);
 }
 
 }  // namespace
