@@ -2,10 +2,6 @@
 // confspec_int4.h.
 #include "kernels.h"
 #include <algorithm>
-#ifdef KV4_TUNE
-#include <cstdlib>
-#include <cstdio>
-#endif
 
 namespace cs {
 
@@ -80,7 +76,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
     const int i = min(max(t - b.cu[trace], 0), b.T - 1), row = min(max(b.plens[trace], 0), b.max_L) + i, slot = row & 15;
     const bool store = (!a.n_append || i < a.n_append[trace]) && row >> 4 < b.max_blocks;
     uint8_t *const pages = page_of(b, trace, row, 0);
-    // theta^(-j / 64) for j = 2 i and 2 i + 1, from its six powers of two (64 values in the arguments would be 2 us away, in host memory)
+    // theta^(-j / 64) for j = 2 i and 2 i + 1, from the six powers theta^(-2^k / 64)
     double f0 = i2 & 1 ? a.theta_pow[1] : 1.0;
 #pragma unroll
     for (int k = 1; k < 5; ++k) f0 *= (i2 >> k) & 1 ? a.theta_pow[k + 1] : 1.0;
@@ -140,22 +136,26 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
 __device__ __forceinline__ float param_s(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p & 0xffff))); }
 __device__ __forceinline__ float param_z(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p >> 16))); }
 
-// A thread has 8 elements (one word) of a key or value row; eight heads of a token a workgroup.
+// Eight heads of a token a workgroup, four at a time: a wavefront has a head's key and value row, a thread half a word of it, so that
+// a wavefront's stores are 512 consecutive bytes twice.
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, float *__restrict__ k, float *__restrict__ v) {
-    const int t = blockIdx.x / n_split, h = blockIdx.x % n_split * 8 + (threadIdx.x >> 5);
-    const int trace = trace_of(b.cu, b.B, t, threadIdx.x & 63);
+    const int t = blockIdx.x / n_split, lane = threadIdx.x & 63, h0 = blockIdx.x % n_split * 8 + (threadIdx.x >> 6);
+    const int trace = trace_of(b.cu, b.B, t, lane);
     const int row = min(max(b.plens[trace], 0), b.max_L) + min(max(t - b.cu[trace], 0), b.T - 1), slot = row & 15;
-    if (h >= b.Hkv) return;
-    const int is_v = (threadIdx.x >> 4) & 1, d = (threadIdx.x & 15) * 8;
-    const uint8_t *page = page_of(b, trace, row, h);
-    const unsigned w = *(const unsigned *)(page + (is_v ? v_word(slot, d) : k_word(slot, d)));
-    const unsigned p = *(const unsigned *)(page + (is_v ? KV4_VP : KV4_KP) + slot * 4);
-    float *dst = (is_v ? v : k) + ((size_t)t * b.Hkv + h) * 128 + d;
-    float x[8];
+    const int is_v = lane >> 5, d = (lane & 31) * 4;
+    const uint8_t *pages = page_of(b, trace, row, 0);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = fmaf(param_s(p), (float)((w >> (is_v ? 4 * e : k_shift(e))) & 15), param_z(p));
-    *(float4 *)dst = make_float4(x[0], x[1], x[2], x[3]);
-    *(float4 *)(dst + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    for (int u = 0; u < 2; ++u) {
+        const int h = h0 + 4 * u;
+        if (h >= b.Hkv) continue;
+        const uint8_t *page = pages + (size_t)h * KV4_PAGE;
+        const unsigned w = *(const unsigned *)(page + (is_v ? v_word(slot, d & ~7) : k_word(slot, d & ~7)));
+        const unsigned p = *(const unsigned *)(page + (is_v ? KV4_VP : KV4_KP) + slot * 4);
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = fmaf(param_s(p), (float)((w >> (is_v ? 4 * ((d & 4) + e) : k_shift((d & 4) + e))) & 15), param_z(p));
+        *(float4 *)((is_v ? v : k) + ((size_t)t * b.Hkv + h) * 128 + d) = make_float4(x[0], x[1], x[2], x[3]);
+    }
 }
 
 // ---- attention ----
@@ -514,8 +514,8 @@ __device__ __forceinline__ int scan64(int v) {               // inclusive sums o
 }
 
 // Where an item of the launch (MERGE: a row of a trace that was cut) lies.  The list is never written out: every wavefront adds the
-// traces' counts up, 64 at a time, from the lengths it needs anyway - a list in the kernel's arguments cost 3 us, which lie in host
-// memory.  What the host counted (same arithmetic: count_items) bounds what is found.
+// traces' counts up, 64 at a time, from the lengths it needs anyway, so that a launch takes 256 traces and no list is copied for it.
+// What the host counted (same arithmetic: count_items) bounds what is found.
 struct Place4 {
     int trace, t0, S, L, P, n_tiles, local, first_record;
     bool found;
@@ -558,15 +558,14 @@ __device__ __forceinline__ Place4 find_item(const Kv4Batch &kv, const AttnPlan4 
 
 constexpr int O_PAD = 132;            // floats from row to row of O in LDS
 
-// WR x WK wavefronts: WR take different rows, WK different chunks of keys.
-template <int NQ, int WR, int WK>
-__global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2 ? 2 : 1) void kv4_attn_kernel(Kv4Attn a, AttnPlan4 plan, float *part_o, float2 *part_ml) {
-    constexpr int ROWS = 16 * NQ * WR, ROWS_LOG2 = __builtin_ctz(ROWS);
-    static_assert((ROWS & (ROWS - 1)) == 0, "");
-    __shared__ float s_o[WK > 1 ? WK * ROWS * O_PAD : 1];
-    __shared__ float2 s_ml[WK > 1 ? WK * ROWS : 1];
+// WK wavefronts have the same rows and take different chunks of keys.
+template <int NQ, int WK>
+__global__ __launch_bounds__(WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_kernel(Kv4Attn a, AttnPlan4 plan, float *part_o, float2 *part_ml) {
+    constexpr int ROWS = 16 * NQ, ROWS_LOG2 = __builtin_ctz(ROWS);
+    __shared__ float s_o[WK * ROWS * O_PAD];
+    __shared__ float2 s_ml[WK * ROWS];
     const Kv4Batch &kv = a.b;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
+    const int tid = threadIdx.x, lane = tid & 63, wk = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n15 = lane & 15, g = lane >> 4;
     unsigned item = blockIdx.x;
     if (plan.swizzle) {               // workgroups are dealt out over 8 L2 caches: neighbours in the list, which share keys, to one
@@ -578,7 +577,7 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2
     if (!f.found) return;             // (only where device and host lengths differ; so are the record's bounds below)
     const int trace = f.trace, t0 = f.t0, S = f.S, L = f.L, n_rows = G * S, n_tiles = f.n_tiles, P = f.P;
     const int rt = f.local % n_tiles, piece = f.local / n_tiles % P, h = f.local / n_tiles / P;
-    const int row0 = rt * ROWS + wr * 16 * NQ;
+    const int row0 = rt * ROWS;
 
     Rows4<NQ> R;
     int tok[NQ], q_row[NQ];
@@ -666,68 +665,56 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WR * WK <= 4 ? 3 : NQ <= 2
     if (c_end > n_cached) {
         const size_t stride = (size_t)kv.Hkv * 128;
         const bf16 *k = a.k + (size_t)t0 * stride + (size_t)h * 128, *v = a.v + (size_t)t0 * stride + (size_t)h * 128;
-        const int my_hi = (min(row0 + 16 * NQ, n_rows) - 1) / G;      // (negative rows cannot be: row0 may lie behind the last row)
         for (; c < c_end; c += WK) {
             const int j0 = 32 * (c - n_cached);
-            if (j0 > my_hi || !suffix_chunk<NQ>(R, a.q, q_row, k, v, stride, j0, S, tok, n15, g)) continue;
-            add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
+            if (suffix_chunk<NQ>(R, a.q, q_row, k, v, stride, j0, S, tok, n15, g)) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
         }
     }
 
-    const bool direct = P == 1;
-    const size_t rec = (size_t)f.first_record + ((size_t)(h * n_tiles + rt) * P + piece);
-    if (!direct && rec >= (size_t)plan.n_records) return;
-    auto store8 = [&](int row_in_tile, int col, const float (&o)[8], float m, float l, bool first) {
-        const int row = rt * ROWS + row_in_tile;
-        if (row >= n_rows) return;
-        if (direct) {
-            const float f = 1.f / l;
-            const u32x4 r = {pack_bf16(o[0] * f, o[1] * f), pack_bf16(o[2] * f, o[3] * f), pack_bf16(o[4] * f, o[5] * f), pack_bf16(o[6] * f, o[7] * f)};
-            *(u32x4 *)(a.out + ((size_t)(t0 + row / G) * a.Hq + h * G + row % G) * 128 + col) = r;
-        } else {
-            float *dst = part_o + (rec * ROWS + row_in_tile) * 128 + col;
-            *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
-            *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
-            if (first) part_ml[rec * ROWS + row_in_tile] = make_float2(m, l);
-        }
-    };
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const float l = sum_over_g(R.l[n]), zs = sum_over_g(R.zs[n]);
-        const int row = wr * 16 * NQ + 16 * n + n15;
+        const int row = 16 * n + n15;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             float o[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = fmaf(R.o[n][j][r], 1.f / (j & 1 ? UNIT_ODD : UNIT_EVEN), zs);
-            if constexpr (WK == 1) {
-                store8(row, 32 * g + 8 * r, o, R.m[n], l, g == 0 && r == 0);
-            } else {
-                float *dst = s_o + (wk * ROWS + row) * O_PAD + 32 * g + 8 * r;
-                *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
-                *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
-                if (g == 0 && r == 0) s_ml[wk * ROWS + row] = make_float2(R.m[n], l);
-            }
+            float *dst = s_o + (wk * ROWS + row) * O_PAD + 32 * g + 8 * r;
+            *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
+            *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
+            if (g == 0 && r == 0) s_ml[wk * ROWS + row] = make_float2(R.m[n], l);
         }
     }
-    if constexpr (WK > 1) {
-        __syncthreads();
-        for (int at = tid; at < ROWS * 16; at += WR * WK * 64) {
-            const int row = at >> 4, col = (at & 15) * 8;
-            float m = M_NONE;
+    __syncthreads();
+    const bool direct = P == 1;
+    const size_t rec = (size_t)f.first_record + ((size_t)(h * n_tiles + rt) * P + piece);
+    if (!direct && rec >= (size_t)plan.n_records) return;
+    for (int at = tid; at < ROWS * 16; at += WK * 64) {
+        const int tile_row = at >> 4, col = (at & 15) * 8, row = row0 + tile_row;
+        if (row >= n_rows) continue;
+        float m = M_NONE;
 #pragma unroll
-            for (int w = 0; w < WK; ++w) m = fmaxf(m, s_ml[w * ROWS + row].x);
-            float l = 0.f, o[8] = {};
+        for (int w = 0; w < WK; ++w) m = fmaxf(m, s_ml[w * ROWS + tile_row].x);
+        float l = 0.f, o[8] = {};
 #pragma unroll
-            for (int w = 0; w < WK; ++w) {
-                const float2 ml = s_ml[w * ROWS + row];
-                const float f = __builtin_amdgcn_exp2f(ml.x - m);
-                l += f * ml.y;
-                const float *src = s_o + (w * ROWS + row) * O_PAD + col;
+        for (int w = 0; w < WK; ++w) {
+            const float2 ml = s_ml[w * ROWS + tile_row];
+            const float f = __builtin_amdgcn_exp2f(ml.x - m);
+            l += f * ml.y;
+            const float *src = s_o + (w * ROWS + tile_row) * O_PAD + col;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] += f * src[e];
-            }
-            store8(row, col, o, m, l, col == 0);
+            for (int e = 0; e < 8; ++e) o[e] += f * src[e];
+        }
+        if (direct) {
+            const float f = 1.f / l;
+            const u32x4 r = {pack_bf16(o[0] * f, o[1] * f), pack_bf16(o[2] * f, o[3] * f), pack_bf16(o[4] * f, o[5] * f), pack_bf16(o[6] * f, o[7] * f)};
+            *(u32x4 *)(a.out + ((size_t)(t0 + row / G) * a.Hq + h * G + row % G) * 128 + col) = r;
+        } else {
+            float *dst = part_o + (rec * ROWS + tile_row) * 128 + col;
+            *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
+            *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
+            if (col == 0) part_ml[rec * ROWS + tile_row] = make_float2(m, l);
         }
     }
 }
@@ -785,8 +772,8 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 pla
 // The launches of a batch: up to ATT_TRACES traces each.
 struct Launch4 {
     AttnPlan4 plan;
-    int nq, wr, wk;
-    int rows_log2() const { return __builtin_ctz(16 * nq * wr); }
+    int nq, wk;
+    int rows_log2() const { return __builtin_ctz(16 * nq); }
     size_t record_rows() const { return (size_t)plan.n_records << rows_log2(); }
 };
 // Pieces are of 32 chunks at least.  With eight wavefronts one workgroup fits a CU, and what does not fit at once waits for a whole item: as
@@ -809,21 +796,15 @@ void plan_launch(Launch4 &p, const int32_t *h_cu, const int32_t *h_lens, int b0,
         units += (int64_t)Hkv * (((int64_t)G * S + 31) / 32);
     }
     p.nq = (int64_t)G * max_S <= 16 || units < 128 ? 1 : 2;
-    p.wr = 1;
     p.wk = units >= 256 ? 4 : 8;
-    int slots = att_slots(p.wk), least = ATT_MIN_CHUNKS;
-#ifdef KV4_TUNE
-    if (getenv("KV4_CFG")) sscanf(getenv("KV4_CFG"), "%d,%d,%d", &p.nq, &p.wr, &p.wk);
-    slots = getenv("KV4_SLOTS") ? atoi(getenv("KV4_SLOTS")) : att_slots(p.wk);
-    if (getenv("KV4_MIN")) least = atoi(getenv("KV4_MIN"));
-#endif
+    const int slots = att_slots(p.wk);
     AttnPlan4 &a = p.plan;
     int64_t total = 0;                // chunks of all tiles
     for (int b = b0; b < b0 + nb; ++b) {
         const int S = h_cu[b + 1] - h_cu[b];
         total += (int64_t)Hkv * (((int64_t)G * S + (1 << p.rows_log2()) - 1) >> p.rows_log2()) * (((int64_t)h_lens[b] + 31) / 32 + (S + 31) / 32);
     }
-    for (int64_t per = std::max<int64_t>(least, (total + slots - 1) / slots);; per += per / 8 + 1) {
+    for (int64_t per = std::max<int64_t>(ATT_MIN_CHUNKS, (total + slots - 1) / slots);; per += per / 8 + 1) {
         a = AttnPlan4{b0, nb, (uint32_t)std::min<int64_t>(per, 1 << 27), 0, 0, 0, 0, 0};
         a.per_inv = (uint32_t)(((1ull << 32) + a.per - 1) / a.per);
         for (int b = b0; b < b0 + nb; ++b) {
@@ -873,15 +854,11 @@ hipError_t launch_kv4_attn(const Kv4Attn &a, const int32_t *h_cu, const int32_t 
         plan_launch(p, h_cu, h_lens, b0, std::min(ATT_TRACES, a.b.B - b0), a.Hq, a.b.Hkv);
         float *part_o = (float *)scratch;
         float2 *part_ml = (float2 *)((char *)scratch + part_o_bytes(p));
-        const int threads = 64 * p.wr * p.wk;
-#ifdef KV4_TUNE
-#define TRY(A, B, C) else if (p.nq == A && p.wr == B && p.wk == C) kv4_attn_kernel<A, B, C><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        if (0) {} TRY(1, 1, 2) TRY(2, 2, 2) TRY(2, 4, 1) TRY(2, 2, 4) TRY(4, 1, 4) else
-#endif
-        if (p.nq == 2 && p.wk == 8) kv4_attn_kernel<2, 1, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        else if (p.nq == 2) kv4_attn_kernel<2, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        else if (p.wk == 4) kv4_attn_kernel<1, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        else kv4_attn_kernel<1, 1, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        const int threads = 64 * p.wk;
+        if (p.nq == 2 && p.wk == 8) kv4_attn_kernel<2, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else if (p.nq == 2) kv4_attn_kernel<2, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else if (p.wk == 4) kv4_attn_kernel<1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else kv4_attn_kernel<1, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
         if (hipError_t e = hipGetLastError()) return e;
         if (p.plan.n_merge_rows) {
             kv4_merge_kernel<<<(p.plan.n_merge_rows + 3) / 4, 256, 0, s>>>(a, p.plan, p.rows_log2(), part_o, part_ml);

@@ -1,7 +1,6 @@
 // Products of up to 128 rows with 4-bit weights.  Record format: confspec_int4.h, kernels.h.
 #include "kernels.h"
 #include <algorithm>
-#include <cstdlib>
 
 namespace cs {
 
@@ -78,7 +77,7 @@ template <> struct Params<1> { typedef unsigned T; static __device__ unsigned ge
 template <> struct Params<2> { typedef uint2 T; static __device__ unsigned get(T p, int g) { return g ? p.y : p.x; } };
 template <> struct Params<4> { typedef u32x4 T; static __device__ unsigned get(T p, int g) { return p[g]; } };
 
-constexpr int max_waves(int MT, int) { return MT == 1 ? 16 : 8; }   // of a workgroup: what the registers of a wavefront leave room for
+constexpr int max_waves(int MT) { return MT == 1 ? 16 : 8; }   // of a workgroup: what the registers of a wavefront leave room for
 
 // Loads of 16, 8 or 4 bytes from a wave-uniform base plus a byte offset per lane; offsets at or past the end read zeros, and
 // touch no memory: so blocks behind the last one need no case of their own.
@@ -99,7 +98,7 @@ struct Block {                        // operands of one block of k as they come
 };
 
 template <int MT, int AL, int NT, int NG, int D>
-__global__ __launch_bounds__(64 * max_waves(MT, NT)) void w4_gemm_kernel(W4Gemm g, int n_mb, int W) {
+__global__ __launch_bounds__(64 * max_waves(MT)) void w4_gemm_kernel(W4Gemm g, int n_mb, int W) {
     extern __shared__ u32x4 s_mem[];
     constexpr int REC = 1024 + 64 * NG;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n15 = lane & 15, kg = lane >> 4;
@@ -225,7 +224,7 @@ hipError_t launch_group(const W4Gemm &a, int W, hipStream_t s) {
     const size_t lds = (size_t)W * MT * 1024 * std::max(4, NT);        // rows of A, then partial sums
     if (lds > 65536) {
         static std::atomic<uint32_t> set{0};
-        if (hipError_t e = set_dynamic_lds_once(set, (const void *)w4_gemm_kernel<MT, AL, NT, NG, D>, max_waves(MT, NT) * MT * 1024 * std::max(4, NT))) return e;
+        if (hipError_t e = set_dynamic_lds_once(set, (const void *)w4_gemm_kernel<MT, AL, NT, NG, D>, max_waves(MT) * MT * 1024 * std::max(4, NT))) return e;
     }
     w4_gemm_kernel<MT, AL, NT, NG, D><<<dim3((unsigned)n_mb * (unsigned)n_nb), dim3(64 * W), lds, s>>>(a, n_mb, W);
     return hipGetLastError();
@@ -282,14 +281,7 @@ W4Tile w4_tile(int M, int N, int K, int group) {
 }
 
 hipError_t launch_w4_gemm(const W4Gemm &a, hipStream_t s) {
-    W4Tile t = w4_tile(a.M, a.N, a.K, a.group);
-#ifdef W4_TUNE
-    if (getenv("W4_MT")) t.mt = atoi(getenv("W4_MT"));
-    if (getenv("W4_NT")) t.nt = atoi(getenv("W4_NT"));
-    if (getenv("W4_W")) t.W = std::min(std::min(atoi(getenv("W4_W")), w4_kblocks(a.K)), max_waves(t.mt, t.nt));
-    if (t.mt > 1 && t.nt < 2) t.nt = 2;
-    if (t.mt == 1 && t.nt > 2) t.nt = 2;
-#endif
+    const W4Tile t = w4_tile(a.M, a.N, a.K, a.group);
     if (t.mt == 1 && a.M <= 4) return t.nt == 1 ? launch<1, 1, 1, 2>(a, t.W, s) : launch<1, 1, 2, 2>(a, t.W, s);
     if (t.mt == 1 && a.M <= 8) return t.nt == 1 ? launch<1, 2, 1, 2>(a, t.W, s) : launch<1, 2, 2, 2>(a, t.W, s);
     if (t.mt == 1) return t.nt == 1 ? launch<1, 4, 1, 2>(a, t.W, s) : launch<1, 4, 2, 2>(a, t.W, s);
