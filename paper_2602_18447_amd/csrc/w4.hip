@@ -91,13 +91,15 @@ struct Loads {
 constexpr unsigned PAST_END = 0x80000000u;
 
 // AL: loads of four rows of A each a block takes, at least as many as there are rows.
-template <int AL, int NT, int NG>
-struct Block {                        // operands of one block of k as they come from memory
-    u32x4 a[AL], w[NT];
+template <int NT, int NG>
+struct BlockW {                       // operands of one block of k as they come from memory
+    u32x4 w[NT];
     typename Params<NG>::T p[NT];
 };
+template <int AL>
+struct BlockA { u32x4 v[AL]; };
 
-template <int MT, int AL, int NT, int NG, int D>
+template <int MT, int AL, int NT, int NG>
 __global__ __launch_bounds__(64 * max_waves(MT)) void w4_gemm_kernel(W4Gemm g, int n_mb, int W) {
     extern __shared__ u32x4 s_mem[];
     constexpr int REC = 1024 + 64 * NG;
@@ -118,10 +120,12 @@ __global__ __launch_bounds__(64 * max_waves(MT)) void w4_gemm_kernel(W4Gemm g, i
     const u32x4 neg16_bits = {0xC180C180u, 0xC180C180u, 0xC180C180u, 0xC180C180u};
     const bf16x8 neg16 = __builtin_bit_cast(bf16x8, neg16_bits);
 
-    auto load = [&](Block<AL, NT, NG> &b, int kb) {
+    auto load_a = [&](BlockA<AL> &b, int kb) {
         const unsigned k = (unsigned)kb * 256u + 16u * n15, at = (int)k < 2 * g.K ? k : PAST_END;      // (K a multiple of 32: 64 bytes)
 #pragma unroll
-        for (int j = 0; j < AL; ++j) A.get(a_at[j] + at, b.a[j]);
+        for (int j = 0; j < AL; ++j) A.get(a_at[j] + at, b.v[j]);
+    };
+    auto load_w = [&](BlockW<NT, NG> &b, int kb) {
         const unsigned rec = kb < n_kb ? (unsigned)kb * REC : PAST_END;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -132,10 +136,12 @@ __global__ __launch_bounds__(64 * max_waves(MT)) void w4_gemm_kernel(W4Gemm g, i
     };
     // Rows of A: 16 lanes have 256 consecutive bytes of a row, the operand wants a row a lane; through LDS, where row r keeps
     // its 16-byte piece v at v ^ r % 16: 16 lanes then meet all banks both ways.
-    auto compute = [&](const Block<AL, NT, NG> &b) {
+    auto stage = [&](const BlockA<AL> &b) {
 #pragma unroll
-        for (int j = 0; j < AL; ++j) s_a[(4 * j + kg) * 16 + (n15 ^ ((4 * j + kg) & 15))] = b.a[j];
+        for (int j = 0; j < AL; ++j) s_a[(4 * j + kg) * 16 + (n15 ^ ((4 * j + kg) & 15))] = b.v[j];
         __builtin_amdgcn_wave_barrier();
+    };
+    auto compute = [&](const BlockW<NT, NG> &b) {
         bf16x8 a[MT][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -169,16 +175,32 @@ __global__ __launch_bounds__(64 * max_waves(MT)) void w4_gemm_kernel(W4Gemm g, i
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    {
-        Block<AL, NT, NG> b[D];       // D - 1 blocks on their way while one is worked on
-#pragma unroll
-        for (int u = 0; u < D - 1; ++u) load(b[u], wave + u * W);
-        for (int kb = wave; kb < n_kb; kb += D * W) {
-#pragma unroll
-            for (int u = 0; u < D; ++u) {
-                load(b[(u + D - 1) % D], kb + (u + D - 1) * W);
-                compute(b[u]);
-            }
+    // One tile of rows: the next block is asked for as soon as A's registers are free, and the registers for W are there twice (with a
+    // second set for A, asked for a block earlier: 8.9 us for 8.1, 16 rows, N = 17920, K = 1536, groups of 64).  More tiles have no registers
+    // for that, nor time to win: 72 rows, N = 7168, K = 5120, groups of 32, tiles of 3 x 2: 23.4 us with, 23.9 without.
+    BlockA<AL> x;
+    BlockW<NT, NG> w0;
+    if constexpr (MT == 1) {
+        BlockW<NT, NG> w1;
+        load_a(x, wave);
+        load_w(w0, wave);
+        for (int kb = wave; kb < n_kb; kb += 2 * W) {
+            stage(x);
+            load_a(x, kb + W);
+            load_w(w1, kb + W);
+            compute(w0);
+            if (kb + W >= n_kb) break;
+            stage(x);
+            load_a(x, kb + 2 * W);
+            load_w(w0, kb + 2 * W);
+            compute(w1);
+        }
+    } else {
+        for (int kb = wave; kb < n_kb; kb += W) {
+            load_a(x, kb);
+            load_w(w0, kb);
+            stage(x);
+            compute(w0);
         }
     }
     f32x4 *const s_part = (f32x4 *)s_mem;
@@ -218,20 +240,20 @@ __global__ __launch_bounds__(64 * max_waves(MT)) void w4_gemm_kernel(W4Gemm g, i
     }
 }
 
-template <int MT, int AL, int NT, int NG, int D>
+template <int MT, int AL, int NT, int NG>
 hipError_t launch_group(const W4Gemm &a, int W, hipStream_t s) {
     const int n_mb = (a.M + 16 * MT - 1) / (16 * MT), n_nb = (a.N / 16 + NT - 1) / NT;
     const size_t lds = (size_t)W * MT * 1024 * std::max(4, NT);        // rows of A, then partial sums
     if (lds > 65536) {
         static std::atomic<uint32_t> set{0};
-        if (hipError_t e = set_dynamic_lds_once(set, (const void *)w4_gemm_kernel<MT, AL, NT, NG, D>, max_waves(MT) * MT * 1024 * std::max(4, NT))) return e;
+        if (hipError_t e = set_dynamic_lds_once(set, (const void *)w4_gemm_kernel<MT, AL, NT, NG>, max_waves(MT) * MT * 1024 * std::max(4, NT))) return e;
     }
-    w4_gemm_kernel<MT, AL, NT, NG, D><<<dim3((unsigned)n_mb * (unsigned)n_nb), dim3(64 * W), lds, s>>>(a, n_mb, W);
+    w4_gemm_kernel<MT, AL, NT, NG><<<dim3((unsigned)n_mb * (unsigned)n_nb), dim3(64 * W), lds, s>>>(a, n_mb, W);
     return hipGetLastError();
 }
-template <int MT, int AL, int NT, int D>
+template <int MT, int AL, int NT>
 hipError_t launch(const W4Gemm &a, int W, hipStream_t s) {
-    return a.group == 128 ? launch_group<MT, AL, NT, 1, D>(a, W, s) : a.group == 64 ? launch_group<MT, AL, NT, 2, D>(a, W, s) : launch_group<MT, AL, NT, 4, D>(a, W, s);
+    return a.group == 128 ? launch_group<MT, AL, NT, 1>(a, W, s) : a.group == 64 ? launch_group<MT, AL, NT, 2>(a, W, s) : launch_group<MT, AL, NT, 4>(a, W, s);
 }
 
 }  // namespace
@@ -282,12 +304,12 @@ W4Tile w4_tile(int M, int N, int K, int group) {
 
 hipError_t launch_w4_gemm(const W4Gemm &a, hipStream_t s) {
     const W4Tile t = w4_tile(a.M, a.N, a.K, a.group);
-    if (t.mt == 1 && a.M <= 4) return t.nt == 1 ? launch<1, 1, 1, 2>(a, t.W, s) : launch<1, 1, 2, 2>(a, t.W, s);
-    if (t.mt == 1 && a.M <= 8) return t.nt == 1 ? launch<1, 2, 1, 2>(a, t.W, s) : launch<1, 2, 2, 2>(a, t.W, s);
-    if (t.mt == 1) return t.nt == 1 ? launch<1, 4, 1, 2>(a, t.W, s) : launch<1, 4, 2, 2>(a, t.W, s);
-    if (t.mt == 2) return t.nt == 2 ? launch<2, 8, 2, 1>(a, t.W, s) : launch<2, 8, 4, 1>(a, t.W, s);
-    if (t.mt == 3) return t.nt == 2 ? launch<3, 12, 2, 1>(a, t.W, s) : launch<3, 12, 4, 1>(a, t.W, s);
-    return launch<4, 16, 4, 1>(a, t.W, s);
+    if (t.mt == 1 && a.M <= 4) return t.nt == 1 ? launch<1, 1, 1>(a, t.W, s) : launch<1, 1, 2>(a, t.W, s);
+    if (t.mt == 1 && a.M <= 8) return t.nt == 1 ? launch<1, 2, 1>(a, t.W, s) : launch<1, 2, 2>(a, t.W, s);
+    if (t.mt == 1) return t.nt == 1 ? launch<1, 4, 1>(a, t.W, s) : launch<1, 4, 2>(a, t.W, s);
+    if (t.mt == 2) return t.nt == 2 ? launch<2, 8, 2>(a, t.W, s) : launch<2, 8, 4>(a, t.W, s);
+    if (t.mt == 3) return t.nt == 2 ? launch<3, 12, 2>(a, t.W, s) : launch<3, 12, 4>(a, t.W, s);
+    return launch<4, 16, 4>(a, t.W, s);
 }
 
 }  // namespace cs
