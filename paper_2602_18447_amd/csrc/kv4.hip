@@ -172,8 +172,9 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, 
 //    a page's value codes lie in memory such that a lane's 16 bytes are those four tokens of eight columns.  Codes enter as
 //    the keys' do, the probability as the half p s; z is added to the row's sum.  The lane has 32 columns of its one query row,
 //    so scaling, sums and output need nothing of other lanes.
-//  * The running reference M of a row is a bound of score + exponent of s (p s is what must fit a half); it is raised,
-//    and what was summed scaled, only where a row goes beyond it by more than 2^8.
+//  * The running reference M of a row is a bound of score + exponent of s (p s is what must fit a half).  A chunk takes it as it is and
+//    looks at the halves that come out; only where one has grown too large, M is raised, what was summed scaled and the chunk's
+//    probabilities taken again.
 //
 // Bound by the cache's bytes when rows are few (136 bytes a token and head), by the vector pipe when they are many.
 constexpr int ATT_TRACES = 256;       // traces of one launch
@@ -219,12 +220,16 @@ __device__ __forceinline__ float sum_over_g(float v) {
 }
 
 constexpr float SCALE_LOG2 = 0.08838834764831845f * 1.4426950408889634f;
-// References: M bounds score + exponent field of s (15 where s is 1), all in powers of two; p = 2^(score - M + REF).
-// Then p s < 2^(M_ROOM + 6) = 2^14 whatever the rows' s are, and a half ends at 2^16; p itself stays below 2^(M_ROOM + REF).
-constexpr float M_NONE = -3e38f, M_ROOM = 8.f, REF = 20.f, E_ONE = 15.f;
-// Scores beyond this are rounded before the reference is taken off: below, a multiply-add does both, whose unrounded product differs
-// from what the reference was rounded from by less than 2^-10.
-constexpr float BIG = 16384.f;
+// References: M bounds score + exponent field of s (15 where s is 1), all in powers of two, where it is raised; p = 2^(score - M + REF).
+// Then p s is below 2^7, whatever the rows' s are; it may grow to W_ROOM = 2^15 (a half ends at 2^16), p (where s is 0) and its sum to
+// L_ROOM, and the suffix's scores beyond M by M_ROOM, before M is raised again.
+constexpr float M_NONE = -3e38f, M_ROOM = 8.f, REF = 20.f, E_ONE = 15.f, L_ROOM = 0x1p60f;
+constexpr _Float16 W_ROOM = 32768;
+// Where scores are beyond BIG, they are rounded before M is taken off (below, a multiply-add does both), M bounds score + E_BIG, whatever s
+// is (p s < 2^14 still), and p is held at 2^(REF - E_BIG).  From 2^27 on, where E_BIG would be lost in M's own rounding, M bounds the score
+// alone, and that hold is what bounds p, for all alike: equal scores keep equal weights.
+constexpr float BIG = 16384.f, E_BIG = 22.f;
+__device__ __forceinline__ float big_bound(float s) { return fabsf(s) < 0x1p27f ? s + E_BIG : s; }
 // Sums of the value product are in units of 2^-24 in even and of 2^-20 in odd columns.
 constexpr float UNIT_EVEN = 1.f / 16777216.f, UNIT_ODD = 1.f / 1048576.f;
 
@@ -265,9 +270,25 @@ __device__ __forceinline__ void raise(Rows4<NQ> &R, const float (&t_max)[NQ]) {
 __device__ __forceinline__ float mix(unsigned p, float a, float b) { return fmaf((float)__builtin_bit_cast(f16x2, p)[0], a, b); }    // s a + b
 __device__ __forceinline__ float mix_z(unsigned p, float a, float b) { return fmaf((float)__builtin_bit_cast(f16x2, p)[1], a, b); }
 
+// p = 2^score of the lane's eight keys of a row, p s as halves, sums of p and p z onto l0 and z0.
+template <typename F>
+__device__ __forceinline__ void probabilities(f16x8 &w, float &l, float &zs, float l0, float z0, const u32x4 (&vp)[2], F score) {
+    l = l0;
+    zs = z0;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float p = __builtin_amdgcn_exp2f(score(x, r));
+            l += p;
+            zs = mix_z(vp[x][r], p, zs);
+            w[4 * x + r] = (_Float16)mix(vp[x][r], p, 0.f);
+        }
+}
+
 // 32 cached tokens, of which the first n_valid count; what is stored for the others may be anything.
 template <int NQ>
-__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g) {
+__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g, bool &big) {
     f32x4 sc[NQ][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -294,67 +315,54 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
 #pragma unroll
                     for (int n = 0; n < NQ; ++n) sc[n][x][r] = -INFINITY;
                 }
-    float t_max[NQ];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) t_max[n] = -INFINITY;
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float e = (float)((vp[x][r] >> 10) & 31u);
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) t_max[n] = fmaxf(t_max[n], fmaf(sc[n][x][r], R.scale[n], e));
-        }
-    bool over = false, big = false;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) big |= fabsf(t_max[n]) > BIG && fabsf(t_max[n]) < INFINITY;
-    big = __any(big);
-    if (big) {
+    // With the references as they are, unless that was too much for a half or an addend of the sums; most chunks end here.
+    f16x8 w[NQ];
+    float l[NQ], zs[NQ];
+    bool over = big;
+    if (!big) {
+        f16x2 top = {0, 0};
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            t_max[n] = -INFINITY;
+            const float ref = REF - R.m[n];
+            probabilities(w[n], l[n], zs[n], R.l[n], R.zs[n], vp, [&](int x, int r) { return fmaf(sc[n][x][r], R.scale[n], ref); });
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) top = __builtin_elementwise_max(top, f16x2{w[n][e], w[n][e + 1]});
+            over |= l[n] > L_ROOM;
+        }
+        over |= top[0] > W_ROOM || top[1] > W_ROOM;
+    }
+    if (__any(over)) {
+#pragma clang fp contract(off)
+        float t_max[NQ], s_max[NQ];
+        bool beyond = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            t_max[n] = s_max[n] = -INFINITY;
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     sc[n][x][r] *= R.scale[n];
+                    s_max[n] = fmaxf(s_max[n], sc[n][x][r]);
                     t_max[n] = fmaxf(t_max[n], sc[n][x][r] + (float)((vp[x][r] >> 10) & 31u));
                 }
+            beyond |= fabsf(t_max[n]) > BIG && t_max[n] > M_NONE;
         }
-    }
+        big |= (bool)__any(beyond);
+        if (big)
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) over |= t_max[n] > R.m[n] + M_ROOM;
-    if (__any(over)) raise<NQ>(R, t_max);
-    if (big) {
+            for (int n = 0; n < NQ; ++n) t_max[n] = big_bound(s_max[n]);
+        raise<NQ>(R, t_max);
+        const float most = big ? REF - E_BIG : INFINITY;
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)   // (an exponent added to such a score may be lost: p s is bounded by itself)
-                    sc[n][x][r] = fminf((sc[n][x][r] - R.m[n]) + REF, M_ROOM + REF - (float)((vp[x][r] >> 10) & 31u));
-    } else {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            const float ref = REF - R.m[n];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sc[n][x][r] = fmaf(sc[n][x][r], R.scale[n], ref);
-        }
+            probabilities(w[n], l[n], zs[n], R.l[n], R.zs[n], vp, [&](int x, int r) { return fminf((sc[n][x][r] - R.m[n]) + REF, most); });
     }
-    f16x8 w[NQ];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float p = __builtin_amdgcn_exp2f(sc[n][x][r]);
-                R.l[n] += p;
-                R.zs[n] = mix_z(vp[x][r], p, R.zs[n]);
-                w[n][4 * x + r] = (_Float16)mix(vp[x][r], p, 0.f);
-            }
+    for (int n = 0; n < NQ; ++n) {
+        R.l[n] = l[n];
+        R.zs[n] = zs[n];
+    }
     unsigned lo[4], hi[4];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -384,7 +392,8 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
 // add_not_finite has to add.
 template <int NQ>
 __device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *q, const int (&q_row)[NQ], const bf16 *k, const bf16 *v, size_t stride, int j0,
-                                             int S, const int (&tok)[NQ], int n15, int g) {
+                                             int S, const int (&tok)[NQ], int n15, int g, bool &big) {
+#pragma clang fp contract(off)
     bf16x8 qb[NQ][4];
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
@@ -409,7 +418,7 @@ __device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *q, const 
         if (j >= S) vw[t] = u32x4{0u, 0u, 0u, 0u};
     }
     float t_max[NQ];
-    bool masked = false;
+    bool masked = false, beyond = false;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         t_max[n] = -INFINITY;
@@ -420,9 +429,12 @@ __device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *q, const 
             for (int r = 0; r < 4; ++r) {
                 const float s = j0 + 16 * x + 4 * g + r <= tok[n] ? sc[n][x][r] * SCALE_LOG2 : -INFINITY;
                 sc[n][x][r] = s;
-                t_max[n] = fmaxf(t_max[n], s + E_ONE);
+                t_max[n] = fmaxf(t_max[n], s);
             }
+        beyond |= fabsf(t_max[n]) > BIG && t_max[n] > M_NONE;
     }
+    big |= (bool)__any(beyond);
+    const float most = big ? REF - E_BIG : INFINITY;
     // A value that is not a finite number may only reach the rows that see its token, but a product takes 0 times it into every
     // row: where rows see a part of the tokens, such values are taken out.
     bool bad = false;
@@ -442,9 +454,12 @@ __device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *q, const 
                     if ((vw[t][e] & 0x7f800000u) == 0x7f800000u) vw[t][e] &= 0xffffu;
                 }
     }
-    bool over = false;
+    bool over = big;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) over |= t_max[n] > R.m[n] + M_ROOM;
+    for (int n = 0; n < NQ; ++n) {
+        t_max[n] = big ? big_bound(t_max[n]) : t_max[n] + E_ONE;
+        over |= t_max[n] > R.m[n] + M_ROOM;
+    }
     if (__any(over)) raise<NQ>(R, t_max);
     u32x4 hi[NQ][2], lo[NQ][2];       // in the units of even and of odd columns
 #pragma unroll
@@ -453,7 +468,8 @@ __device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *q, const 
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int r = 0; r < 4; r += 2) {
-                const float p0 = __builtin_amdgcn_exp2f((sc[n][x][r] - R.m[n]) + REF), p1 = __builtin_amdgcn_exp2f((sc[n][x][r + 1] - R.m[n]) + REF);
+                const float p0 = __builtin_amdgcn_exp2f(fminf((sc[n][x][r] - R.m[n]) + REF, most));
+                const float p1 = __builtin_amdgcn_exp2f(fminf((sc[n][x][r + 1] - R.m[n]) + REF, most));
                 R.l[n] += p0;
                 R.l[n] += p1;
 #pragma unroll
@@ -618,6 +634,7 @@ __global__ __launch_bounds__(WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_
     const int n_cached = (L + 31) >> 5, tok_hi = (min((rt + 1) * ROWS, n_rows) - 1) / G, n_all = n_cached + (tok_hi >> 5) + 1;
     const int c_begin = (int)((int64_t)n_all * piece / P), c_end = (int)((int64_t)n_all * (piece + 1) / P);
     const int c_stop = min(c_end, n_cached);
+    bool big = false;                 // scores beyond BIG were met
     if (c_begin + wk < c_stop) {
         const int32_t *table = kv.table + (size_t)trace * kv.max_blocks;
         const uint8_t *head = kv.pages + (size_t)h * KV4_PAGE;
@@ -643,7 +660,7 @@ __global__ __launch_bounds__(WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_
             __builtin_amdgcn_sched_barrier(0);   // (loads stay ahead of the products before them in time)
         };
         auto compute = [&](const Chunk4 &d, int i) {
-            cached_chunk<NQ>(R, d, L - 32 * (c_begin + wk + WK * i), g);
+            cached_chunk<NQ>(R, d, L - 32 * (c_begin + wk + WK * i), g, big);
             __builtin_amdgcn_sched_barrier(0);
         };
         const int n = (c_stop - c_begin - wk + WK - 1) / WK;
@@ -667,7 +684,7 @@ __global__ __launch_bounds__(WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_
         const bf16 *k = a.k + (size_t)t0 * stride + (size_t)h * 128, *v = a.v + (size_t)t0 * stride + (size_t)h * 128;
         for (; c < c_end; c += WK) {
             const int j0 = 32 * (c - n_cached);
-            if (suffix_chunk<NQ>(R, a.q, q_row, k, v, stride, j0, S, tok, n15, g)) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
+            if (suffix_chunk<NQ>(R, a.q, q_row, k, v, stride, j0, S, tok, n15, g, big)) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
         }
     }
 

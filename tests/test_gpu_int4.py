@@ -373,6 +373,51 @@ def test_attention_equal_scores_in_long_rows():
         _attn_check(ctx, c, 4, 1, z, z[:, :1].contiguous(), (z[:, :1] + 0.25).contiguous())
 
 
+@pytest.mark.parametrize("L, S", [((70, 0, 33), (1, 3, 40)), ((5003,), (2,))])
+def test_attention_equal_scores_of_any_size(L, S):
+    """Keys all equal (0.5 everywhere), queries of one element, up to 2^100: every score is the same product, in the cache and in the
+    suffix, and weights are even however large it is and whatever the value rows' s are."""
+    gen = _gen(43)
+    Hq, Hkv = 16, 2
+    c = Cache(gen, Hkv, L, S)
+    n = c.pages[0].shape[0] * Hkv
+    page = c.pages.view(n, R.PAGE)
+    page[:, :1024] = 0
+    half = torch.zeros(n, 16, 2, dtype=torch.float16, device=DEV)
+    half[:, :, 1] = 0.5
+    page[:, 2048:2112] = half.view(n, 32).view(torch.uint8)
+    par = page[:, 2112:2176].contiguous().view(torch.float16).view(n, 16, 2)
+    par[:, :, 0] *= 2.0 ** torch.randint(-6, 7, (n, 16), generator=gen, device=DEV).half()
+    page[:, 2112:2176] = par.view(n, 32).view(torch.uint8)
+    q = torch.zeros(c.T, Hq, 128, device=DEV)
+    size = [0, 5, 12, 14, 16, 18, 22, 25, 28, 31, 36, 50, 70, 100]
+    for h in range(Hq):
+        for t in range(c.T):
+            q[t, h, (7 * t + h) % 128] = (-1.0) ** (t + h // 2) * 2.0 ** size[(3 * t + h) % len(size)]
+    k = torch.full((c.T, Hkv, 128), 0.5, device=DEV).bfloat16()
+    v = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV).bfloat16()
+    out = torch.empty(c.T, Hq * 128, dtype=torch.bfloat16, device=DEV)
+    with Ctx(Hq, Hkv) as ctx:
+        cb.confspec_op_kv4_attention(ctx, c.kv, c.batch, 0, q.bfloat16(), k, v, out, c.scratch(ctx))
+    for b, (l, s) in enumerate(zip(L, S)):
+        ids = torch.as_tensor(c.table[b][:(l + 15) // 16].astype(np.int64), device=DEV)
+        for h in range(Hkv):
+            vc, vs, vz = R.read_pages(c.pages[0][ids, h])[1] if l else (torch.zeros(0, 16, 128, device=DEV).double(),) + (torch.zeros(0, 16, device=DEV).double(),) * 2
+            sc = (vs[..., None] * vc).reshape(-1, 128)[:l]
+            z = vz.reshape(-1)[:l, None].expand(-1, 128)
+            for i in range(s):
+                t = int(c.cu[b]) + i
+                suffix = v[int(c.cu[b]):t + 1, h].double()
+                m = l + i + 1
+                want = (sc.sum(0) + z.sum(0) + suffix.sum(0)) / m
+                apart = (sc.sum(0) + z.abs().sum(0) + suffix.abs().sum(0)) / m
+                # half a step of the result; of p s as a half, whose smallest step is 2^-24 for p = 2^-2; scores below 2^14 are rounded
+                # to 2^-11 in the suffix and not in the cache; sums
+                tol = 2.0 ** -8 * want.abs() + 2.0 ** -11 * sc.sum(0) / m + 15 * 2.0 ** -23 + (2.0 ** -10 + (m / 32 + 64) * 2.0 ** -24 * 6) * apart
+                got = out[t].view(Hkv, Hq // Hkv, 128)[h].double()
+                assert bool(((got - want).abs() <= tol).all()), (b, h, i, float(((got - want).abs() / tol).max()))
+
+
 def test_attention_a_nan_stays_in_its_head():
     gen = _gen(18)
     Hq, Hkv = 8, 2
