@@ -230,8 +230,8 @@ constexpr _Float16 W_ROOM = 32768;
 // alone, and that hold is what bounds p, for all alike: equal scores keep equal weights.
 constexpr float BIG = 16384.f, E_BIG = 22.f;
 __device__ __forceinline__ float big_bound(float s) { return fabsf(s) < 0x1p27f ? s + E_BIG : s; }
-// Sums of the value product are in units of 2^-24 in even and of 2^-20 in odd columns.
-constexpr float UNIT_EVEN = 1.f / 16777216.f, UNIT_ODD = 1.f / 1048576.f;
+// Sums of the cached tokens' value product are of so many units in even and in odd columns.
+constexpr float EVEN_UNITS = 16777216.f, ODD_UNITS = 1048576.f;
 
 // Loads of 16 bytes from a wave-uniform base plus a byte offset per lane; offsets at or past the end read zeros.
 struct Loads {
@@ -387,125 +387,15 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
     }
 }
 
-// 32 suffix tokens from j0 on; k, v point at the trace's first token and the head, rows are `stride` elements apart; a row
-// sees tokens up to its own (tok).  Products in bfloat16, probabilities in two terms.  True: values were taken out that
-// add_not_finite has to add.
-template <int NQ>
-__device__ __forceinline__ bool suffix_chunk(Rows4<NQ> &R, const bf16 *q, const int (&q_row)[NQ], const bf16 *k, const bf16 *v, size_t stride, int j0,
-                                             int S, const int (&tok)[NQ], int n15, int g, bool &big) {
-#pragma clang fp contract(off)
-    bf16x8 qb[NQ][4];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) qb[n][i] = *(const bf16x8 *)(q + (size_t)q_row[n] * 128 + 8 * g + 32 * i);
-    f32x4 sc[NQ][2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const bf16 *row = k + (size_t)min(j0 + 16 * x + n15, S - 1) * stride + 8 * g;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bf16x8 a = *(const bf16x8 *)(row + 32 * i);
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) sc[n][x] = mma(a, qb[n][i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[n][x]);
-        }
-    }
-    u32x4 vw[8];
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        const int j = j0 + 16 * (t >> 2) + 4 * g + (t & 3);
-        vw[t] = *(const u32x4 *)(v + (size_t)min(j, S - 1) * stride + 8 * n15);
-        if (j >= S) vw[t] = u32x4{0u, 0u, 0u, 0u};
-    }
-    float t_max[NQ];
-    bool masked = false, beyond = false;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        t_max[n] = -INFINITY;
-        masked |= j0 + 31 > tok[n];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float s = j0 + 16 * x + 4 * g + r <= tok[n] ? sc[n][x][r] * SCALE_LOG2 : -INFINITY;
-                sc[n][x][r] = s;
-                t_max[n] = fmaxf(t_max[n], s);
-            }
-        beyond |= fabsf(t_max[n]) > BIG && t_max[n] > M_NONE;
-    }
-    big |= (bool)__any(beyond);
-    const float most = big ? REF - E_BIG : INFINITY;
-    // A value that is not a finite number may only reach the rows that see its token, but a product takes 0 times it into every
-    // row: where rows see a part of the tokens, such values are taken out.
-    bool bad = false;
-    if (__any(masked)) {
-        unsigned any = 0;
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) any |= (vw[t][e] & 0x7fff7fffu) + 0x00800080u;      // a full exponent carries into the sign's place
-        bad = __any((any & 0x80008000u) != 0u);
-        if (bad)
-#pragma unroll
-            for (int t = 0; t < 8; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if ((vw[t][e] & 0x7f80u) == 0x7f80u) vw[t][e] &= 0xffff0000u;
-                    if ((vw[t][e] & 0x7f800000u) == 0x7f800000u) vw[t][e] &= 0xffffu;
-                }
-    }
-    bool over = big;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        t_max[n] = big ? big_bound(t_max[n]) : t_max[n] + E_ONE;
-        over |= t_max[n] > R.m[n] + M_ROOM;
-    }
-    if (__any(over)) raise<NQ>(R, t_max);
-    u32x4 hi[NQ][2], lo[NQ][2];       // in the units of even and of odd columns
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 4; r += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(fminf((sc[n][x][r] - R.m[n]) + REF, most));
-                const float p1 = __builtin_amdgcn_exp2f(fminf((sc[n][x][r + 1] - R.m[n]) + REF, most));
-                R.l[n] += p0;
-                R.l[n] += p1;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const float a0 = p0 * (u ? UNIT_ODD : UNIT_EVEN), a1 = p1 * (u ? UNIT_ODD : UNIT_EVEN);
-                    const unsigned h = pack_bf16(a0, a1);
-                    hi[n][u][2 * x + (r >> 1)] = h;
-                    lo[n][u][2 * x + (r >> 1)] = pack_bf16(a0 - __uint_as_float(h << 16), a1 - __uint_as_float(h & 0xffff0000u));
-                }
-            }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        u32x4 a;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            a[r] = j & 1 ? hi_halves(vw[2 * r][j >> 1], vw[2 * r + 1][j >> 1]) : lo_halves(vw[2 * r][j >> 1], vw[2 * r + 1][j >> 1]);
-        const bf16x8 av = __builtin_bit_cast(bf16x8, a);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, hi[n][j & 1]), R.o[n][j]);
-            R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, lo[n][j & 1]), R.o[n][j]);
-        }
-    }
-    return bad;
-}
-
-// Adds the values that suffix_chunk took out of tokens j_begin .. j_end - 1 to the rows that see them.  A probability is positive,
+// Adds the values that attend_suffix takes out of tokens j_begin .. j_end - 1 to the rows that see them.  A probability is positive,
 // so that an infinity or NaN is what its column becomes, whatever the probability.
 template <int NQ>
-__device__ __forceinline__ void add_not_finite(Rows4<NQ> &R, const bf16 *v, size_t stride, int j_begin, int j_end, const int (&tok)[NQ], int g) {
+__device__ __forceinline__ void add_not_finite(Rows4<NQ> &R, const bf16 *v, unsigned stride, int j_begin, int j_end, const int (&tok)[NQ], int g) {
 #pragma unroll 1
     for (int j = j_begin; j < j_end; ++j) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const u32x4 w = *(const u32x4 *)(v + (size_t)j * stride + 32 * g + 8 * r);
+            const u32x4 w = *(const u32x4 *)(v + (uint64_t)(unsigned)j * stride + 32 * g + 8 * r);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const unsigned bits = e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16;
@@ -515,6 +405,136 @@ __device__ __forceinline__ void add_not_finite(Rows4<NQ> &R, const bf16 *v, size
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+    }
+}
+
+// Suffix tokens, 32 from j0 on, then from j0 + j_step, below j_end; k, v point at the trace's first token and the head, rows are `stride`
+// elements apart; a row sees tokens up to its own (tok).  Products in bfloat16, probabilities in two terms; R.o is in units of 1.
+// Values are asked for before the scores are taken, the next keys as soon as the registers of these are free.
+template <int NQ>
+__device__ __forceinline__ void attend_suffix(Rows4<NQ> &R, bool &big, const bf16 *q, const int (&q_row)[NQ], const bf16 *k, const bf16 *v, unsigned stride,
+                                              int j0, int j_step, int j_end, int S, const int (&tok)[NQ], int n15, int g) {
+    bf16x8 qb[NQ][4], kb[2][4];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qb[n][i] = *(const bf16x8 *)(q + (size_t)q_row[n] * 128 + 8 * g + 32 * i);
+    auto load_k = [&](int j) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) kb[x][i] = *(const bf16x8 *)(k + (uint64_t)(unsigned)min(j + 16 * x + n15, S - 1) * stride + 8 * g + 32 * i);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    load_k(j0);
+#pragma unroll 1
+    for (; j0 < j_end; j0 += j_step) {
+        u32x4 vw[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) vw[t] = *(const u32x4 *)(v + (uint64_t)(unsigned)min(j0 + 16 * (t >> 2) + 4 * g + (t & 3), S - 1) * stride + 8 * n15);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 sc[NQ][2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) sc[n][x] = mma(kb[x][i], qb[n][i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[n][x]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (j0 + j_step < j_end) load_k(j0 + j_step);
+        // A value that is not a finite number may only reach the rows that see its token, but a product takes 0 times it into every
+        // row: where rows see a part of the tokens, such values are taken out, and added in the end.
+        bool masked = false, bad = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) masked |= j0 + 31 > tok[n];
+        if (__any(masked)) {
+            unsigned any = 0;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const int j = j0 + 16 * (t >> 2) + 4 * g + (t & 3);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+                    if (j > tok[n]) sc[n][t >> 2][t & 3] = -INFINITY;
+                if (j >= S) vw[t] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any |= (vw[t][e] & 0x7fff7fffu) + 0x00800080u;      // a full exponent carries into the sign's place
+            }
+            bad = __any((any & 0x80008000u) != 0u);
+            if (bad)
+#pragma unroll
+                for (int t = 0; t < 8; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if ((vw[t][e] & 0x7f80u) == 0x7f80u) vw[t][e] &= 0xffff0000u;
+                        if ((vw[t][e] & 0x7f800000u) == 0x7f800000u) vw[t][e] &= 0xffffu;
+                    }
+        }
+        float t_max[NQ];
+        bool beyond = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            t_max[n] = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) t_max[n] = fmaxf(t_max[n], sc[n][x][r]);
+            t_max[n] *= SCALE_LOG2;
+            beyond |= fabsf(t_max[n]) > BIG && t_max[n] > M_NONE;
+        }
+        big |= (bool)__any(beyond);
+        bool over = big;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            t_max[n] = big ? big_bound(t_max[n]) : t_max[n] + E_ONE;
+            over |= t_max[n] > R.m[n] + M_ROOM;
+        }
+        if (__any(over)) raise<NQ>(R, t_max);
+        if (big) {
+#pragma clang fp contract(off)
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sc[n][x][r] = fminf((sc[n][x][r] * SCALE_LOG2 - R.m[n]) + REF, REF - E_BIG);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const float ref = REF - R.m[n];
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sc[n][x][r] = fmaf(sc[n][x][r], SCALE_LOG2, ref);
+            }
+        }
+        u32x4 hi[NQ], lo[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(sc[n][x][r]), p1 = __builtin_amdgcn_exp2f(sc[n][x][r + 1]);
+                    R.l[n] += p0;
+                    R.l[n] += p1;
+                    const unsigned h = pack_bf16(p0, p1);
+                    hi[n][2 * x + (r >> 1)] = h;
+                    lo[n][2 * x + (r >> 1)] = pack_bf16(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+                }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            u32x4 a;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                a[r] = j & 1 ? hi_halves(vw[2 * r][j >> 1], vw[2 * r + 1][j >> 1]) : lo_halves(vw[2 * r][j >> 1], vw[2 * r + 1][j >> 1]);
+            const bf16x8 av = __builtin_bit_cast(bf16x8, a);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, hi[n]), R.o[n][j]);
+                R.o[n][j] = mma(av, __builtin_bit_cast(bf16x8, lo[n]), R.o[n][j]);
+            }
+        }
+        if (bad) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
     }
 }
 
@@ -574,14 +594,14 @@ __device__ __forceinline__ Place4 find_item(const Kv4Batch &kv, const AttnPlan4 
 
 constexpr int O_PAD = 132;            // floats from row to row of O in LDS
 
-// WK wavefronts have the same rows and take different chunks of keys.
-template <int NQ, int WK>
-__global__ __launch_bounds__(WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_kernel(Kv4Attn a, AttnPlan4 plan, float *part_o, float2 *part_ml) {
-    constexpr int ROWS = 16 * NQ, ROWS_LOG2 = __builtin_ctz(ROWS);
-    __shared__ float s_o[WK * ROWS * O_PAD];
-    __shared__ float2 s_ml[WK * ROWS];
+// WR x WK wavefronts: WR have different rows, WK of the same rows take different chunks of keys.
+template <int NQ, int WR, int WK>
+__global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_kernel(Kv4Attn a, AttnPlan4 plan, float *part_o, float2 *part_ml) {
+    constexpr int ROWS = 16 * NQ * WR, ROWS_LOG2 = __builtin_ctz(ROWS);
+    __shared__ float s_o[WK > 1 ? WK * ROWS * O_PAD : 1];
+    __shared__ float2 s_ml[WK > 1 ? WK * ROWS : 1];
     const Kv4Batch &kv = a.b;
-    const int tid = threadIdx.x, lane = tid & 63, wk = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave / WK, wk = wave % WK;
     const int n15 = lane & 15, g = lane >> 4;
     unsigned item = blockIdx.x;
     if (plan.swizzle) {               // workgroups are dealt out over 8 L2 caches: neighbours in the list, which share keys, to one
@@ -593,7 +613,7 @@ __global__ __launch_bounds__(WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_
     if (!f.found) return;             // (only where device and host lengths differ; so are the record's bounds below)
     const int trace = f.trace, t0 = f.t0, S = f.S, L = f.L, n_rows = G * S, n_tiles = f.n_tiles, P = f.P;
     const int rt = f.local % n_tiles, piece = f.local / n_tiles % P, h = f.local / n_tiles / P;
-    const int row0 = rt * ROWS;
+    const int row0 = rt * ROWS + wr * 16 * NQ;
 
     Rows4<NQ> R;
     int tok[NQ], q_row[NQ];
@@ -677,52 +697,23 @@ __global__ __launch_bounds__(WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_
             if (i + 1 < n) compute(c1, i + 1);
         }
     }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) R.o[n][j] *= j & 1 ? ODD_UNITS : EVEN_UNITS;
     int c = c_begin + wk;
     if (c < c_stop) c += (c_stop - c + WK - 1) / WK * WK;
-    if (c_end > n_cached) {
-        const size_t stride = (size_t)kv.Hkv * 128;
-        const bf16 *k = a.k + (size_t)t0 * stride + (size_t)h * 128, *v = a.v + (size_t)t0 * stride + (size_t)h * 128;
-        for (; c < c_end; c += WK) {
-            const int j0 = 32 * (c - n_cached);
-            if (suffix_chunk<NQ>(R, a.q, q_row, k, v, stride, j0, S, tok, n15, g, big)) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
-        }
-    }
+    const int c_last = min(c_end, n_cached + (min(row0 + 16 * NQ, n_rows) - 1) / G / 32 + 1);      // (as far as this wavefront's rows see)
+    if (c < c_last)
+        attend_suffix<NQ>(R, big, a.q, q_row, a.k + ((size_t)t0 * kv.Hkv + h) * 128, a.v + ((size_t)t0 * kv.Hkv + h) * 128, kv.Hkv * 128, 32 * (c - n_cached), 32 * WK,
+                          32 * (c_last - n_cached), S, tok, n15, g);
 
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const float l = sum_over_g(R.l[n]), zs = sum_over_g(R.zs[n]);
-        const int row = 16 * n + n15;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float o[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = fmaf(R.o[n][j][r], 1.f / (j & 1 ? UNIT_ODD : UNIT_EVEN), zs);
-            float *dst = s_o + (wk * ROWS + row) * O_PAD + 32 * g + 8 * r;
-            *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
-            *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
-            if (g == 0 && r == 0) s_ml[wk * ROWS + row] = make_float2(R.m[n], l);
-        }
-    }
-    __syncthreads();
     const bool direct = P == 1;
     const size_t rec = (size_t)f.first_record + ((size_t)(h * n_tiles + rt) * P + piece);
     if (!direct && rec >= (size_t)plan.n_records) return;
-    for (int at = tid; at < ROWS * 16; at += WK * 64) {
-        const int tile_row = at >> 4, col = (at & 15) * 8, row = row0 + tile_row;
-        if (row >= n_rows) continue;
-        float m = M_NONE;
-#pragma unroll
-        for (int w = 0; w < WK; ++w) m = fmaxf(m, s_ml[w * ROWS + tile_row].x);
-        float l = 0.f, o[8] = {};
-#pragma unroll
-        for (int w = 0; w < WK; ++w) {
-            const float2 ml = s_ml[w * ROWS + tile_row];
-            const float f = __builtin_amdgcn_exp2f(ml.x - m);
-            l += f * ml.y;
-            const float *src = s_o + (w * ROWS + tile_row) * O_PAD + col;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] += f * src[e];
-        }
+    auto store8 = [&](int tile_row, int col, const float (&o)[8], float m, float l, bool first) {
+        const int row = rt * ROWS + tile_row;
+        if (row >= n_rows) return;
         if (direct) {
             const float f = 1.f / l;
             const u32x4 r = {pack_bf16(o[0] * f, o[1] * f), pack_bf16(o[2] * f, o[3] * f), pack_bf16(o[4] * f, o[5] * f), pack_bf16(o[6] * f, o[7] * f)};
@@ -731,7 +722,46 @@ __global__ __launch_bounds__(WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_attn_
             float *dst = part_o + (rec * ROWS + tile_row) * 128 + col;
             *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
             *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
-            if (col == 0) part_ml[rec * ROWS + tile_row] = make_float2(m, l);
+            if (first) part_ml[rec * ROWS + tile_row] = make_float2(m, l);
+        }
+    };
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const float l = sum_over_g(R.l[n]), zs = sum_over_g(R.zs[n]);
+        const int row = wr * 16 * NQ + 16 * n + n15;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = R.o[n][j][r] + zs;
+            if constexpr (WK == 1) {
+                store8(row, 32 * g + 8 * r, o, R.m[n], l, g == 0 && r == 0);
+            } else {
+                float *dst = s_o + (wk * ROWS + row) * O_PAD + 32 * g + 8 * r;
+                *(f32x4 *)dst = f32x4{o[0], o[1], o[2], o[3]};
+                *(f32x4 *)(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
+                if (g == 0 && r == 0) s_ml[wk * ROWS + row] = make_float2(R.m[n], l);
+            }
+        }
+    }
+    if constexpr (WK > 1) {
+        __syncthreads();
+        for (int at = tid; at < ROWS * 16; at += WR * WK * 64) {
+            const int tile_row = at >> 4, col = (at & 15) * 8;
+            float m = M_NONE;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) m = fmaxf(m, s_ml[w * ROWS + tile_row].x);
+            float l = 0.f, o[8] = {};
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const float2 ml = s_ml[w * ROWS + tile_row];
+                const float f = __builtin_amdgcn_exp2f(ml.x - m);
+                l += f * ml.y;
+                const float *src = s_o + (w * ROWS + tile_row) * O_PAD + col;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] += f * src[e];
+            }
+            store8(tile_row, col, o, m, l, col == 0);
         }
     }
 }
@@ -789,8 +819,8 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 pla
 // The launches of a batch: up to ATT_TRACES traces each.
 struct Launch4 {
     AttnPlan4 plan;
-    int nq, wk;
-    int rows_log2() const { return __builtin_ctz(16 * nq); }
+    int nq, wr, wk;
+    int rows_log2() const { return __builtin_ctz(16 * nq * wr); }
     size_t record_rows() const { return (size_t)plan.n_records << rows_log2(); }
 };
 // Pieces are of 32 chunks at least.  With eight wavefronts one workgroup fits a CU, and what does not fit at once waits for a whole item: as
@@ -801,19 +831,25 @@ constexpr int att_slots(int wk) { return wk == 8 ? 256 : 1536; }
 
 // Rows of a wavefront and wavefronts that share the keys.  32 rows halve the unpacking for each, 16 make more wavefronts; eight
 // wavefronts finish an item sooner, four leave a batch with many items less to merge.  Measured, us (16 rows x 4, 16 x 8, 32 x 4, 32 x 8):
-// 96 tokens on one context of 4096, 12 heads on 2: 15.9, 14.7, 16.3, 16.6;  32 traces of 1 to 7 tokens: 21.9, 20.5, 24, 22.6;  16 traces
-// of 32 to 256 tokens: 228, -, 141, 180;  48 traces of one token, 40 heads on 8: 99, 104.
+// 96 tokens on one context of 4096, 12 heads on 2: 16.8, 16.0, -, -;  32 traces of 1 to 7 tokens: 22.2, 21.4, -, -;  16 traces of 32 to 256
+// tokens: 147, 210, 139, 169;  48 traces of one token, 40 heads on 8: 100, 111, -, -.
+// Where no row has more than 16 chunks of keys and rows are many, sharing them costs more than it brings: four wavefronts of 32 rows each (32 x 4 and these):
+// 64 traces of 100 to 256 tokens on 10 to 100, 12 heads on 2: 87, 55;  16 of 128 on 16: 20.8, 14.6;  32 of 20 to 100 on 100 to 900 (17
+// chunks): 28.9, 32.9;  16 of 8 to 24 on 50 to 300, 40 heads on 8 (384 tiles): 12.4, 16.0.
 void plan_launch(Launch4 &p, const int32_t *h_cu, const int32_t *h_lens, int b0, int nb, int Hq, int Hkv) {
     const int G = Hq / Hkv;
     int max_S = 0;
-    int64_t units = 0;                // tiles of 32 rows
+    int64_t units = 0, most = 0;      // tiles of 32 rows, chunks of the longest
     for (int b = b0; b < b0 + nb; ++b) {
         const int S = h_cu[b + 1] - h_cu[b];
         max_S = std::max(max_S, S);
         units += (int64_t)Hkv * (((int64_t)G * S + 31) / 32);
+        most = std::max(most, ((int64_t)h_lens[b] + 31) / 32 + (S + 31) / 32);
     }
     p.nq = (int64_t)G * max_S <= 16 || units < 128 ? 1 : 2;
     p.wk = units >= 256 ? 4 : 8;
+    p.wr = 1;
+    if (p.nq == 2 && units >= 512 && most <= 16) p.wr = 4, p.wk = 1;
     const int slots = att_slots(p.wk);
     AttnPlan4 &a = p.plan;
     int64_t total = 0;                // chunks of all tiles
@@ -831,7 +867,7 @@ void plan_launch(Launch4 &p, const int32_t *h_cu, const int32_t *h_lens, int b0,
             a.n_merge_rows += c.merge_rows;
             a.swizzle |= c.tiles > 1;
         }
-        if (p.wk == 4 || a.n_items <= slots || a.n_records == 0) break;
+        if (p.wk != 8 || a.n_items <= slots || a.n_records == 0) break;
     }
 }
 
@@ -871,11 +907,12 @@ hipError_t launch_kv4_attn(const Kv4Attn &a, const int32_t *h_cu, const int32_t 
         plan_launch(p, h_cu, h_lens, b0, std::min(ATT_TRACES, a.b.B - b0), a.Hq, a.b.Hkv);
         float *part_o = (float *)scratch;
         float2 *part_ml = (float2 *)((char *)scratch + part_o_bytes(p));
-        const int threads = 64 * p.wk;
-        if (p.nq == 2 && p.wk == 8) kv4_attn_kernel<2, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        else if (p.nq == 2) kv4_attn_kernel<2, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        else if (p.wk == 4) kv4_attn_kernel<1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
-        else kv4_attn_kernel<1, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        const int threads = 64 * p.wr * p.wk;
+        if (p.wr == 4) kv4_attn_kernel<2, 4, 1><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else if (p.nq == 2 && p.wk == 8) kv4_attn_kernel<2, 1, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else if (p.nq == 2) kv4_attn_kernel<2, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else if (p.wk == 4) kv4_attn_kernel<1, 1, 4><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
+        else kv4_attn_kernel<1, 1, 8><<<p.plan.n_items, threads, 0, s>>>(a, p.plan, part_o, part_ml);
         if (hipError_t e = hipGetLastError()) return e;
         if (p.plan.n_merge_rows) {
             kv4_merge_kernel<<<(p.plan.n_merge_rows + 3) / 4, 256, 0, s>>>(a, p.plan, p.rows_log2(), part_o, part_ml);

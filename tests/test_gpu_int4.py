@@ -301,6 +301,12 @@ def test_attention_ragged_batches(seed):
     _attn_case(Hq, Hkv, L, S, seed)
 
 
+@pytest.mark.parametrize("Hq, Hkv, L, S", [(40, 8, (0, 1, 16, 31, 33, 100, 290, 5), (60, 64, 33, 97, 128, 65, 64, 160)), (34, 2, (70,) * 12, tuple(range(30, 54, 2))),
+                                           (4, 4, (0, 64, 200), (256, 300, 312)), (8, 8, (200,) * 40, (20, 65) * 20)])
+def test_attention_many_rows_on_few_keys(Hq, Hkv, L, S):
+    _attn_case(Hq, Hkv, L, S, 18)
+
+
 @pytest.mark.parametrize("L, S", [((40000,), (1,)), ((20000, 5), (2, 3)), ((9000,), (150,)), ((0, 10), (400, 300))])
 def test_attention_long(L, S):
     _attn_case(6, 1, L, S, 11)
@@ -464,6 +470,30 @@ def test_attention_what_a_later_token_holds_stays_out(Hq, Hkv, S, bad):
         seen[at:S, (Hkv - 1) * G:, slice(77, 78) if name == "v" else slice(None)] = True
         assert torch.equal(out[~seen], good[~seen])
         assert not bool(torch.isfinite(out[seen]).any())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_attention_what_a_later_token_holds_stays_out_of_many_rows(bad):
+    """The same where four wavefronts have 32 rows each, and chunks of keys that some of them see as a whole."""
+    gen = _gen(44)
+    Hq, Hkv, S = 40, 8, 100
+    c = Cache(gen, Hkv, (20,) * 6, (S,) * 6)
+    q = torch.randn(c.T, Hq, 128, generator=gen, device=DEV).bfloat16()
+    k = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV).bfloat16()
+    v = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV).bfloat16()
+    outs = []
+    with Ctx(Hq, Hkv) as ctx:
+        for at in (None, 2 * S + 45):
+            if at is not None:
+                v[at, 3, 77] = bad
+            out = torch.empty(c.T, Hq, 128, dtype=torch.bfloat16, device=DEV)
+            cb.confspec_op_kv4_attention(ctx, c.kv, c.batch, 0, q, k, v, out, c.scratch(ctx))
+            outs.append(out)
+        torch.cuda.synchronize()
+    seen = torch.zeros(c.T, Hq, 128, dtype=torch.bool, device=DEV)
+    seen[2 * S + 45:3 * S, 15:20, 77] = True
+    assert torch.equal(outs[1][~seen], outs[0][~seen])
+    assert not bool(torch.isfinite(outs[1][seen]).any())
 
 
 def test_cache_beyond_4_gib():
