@@ -386,16 +386,18 @@ W4_MAX_ROWS = 128
 KV4_PAGE_BYTES = 2176
 
 
-def _host_i32(a):
-    """(address, what has to live during the call) of host int32 values.  A contiguous int32 array is read where it is, by way of
+def _host_i32(a, n: int):
+    """(address, what has to live during the call) of n host int32 values.  A contiguous int32 array is read where it is, by way of
     its buffer: asking numpy for the address takes longer than the launch's checks."""
     try:
-        if a.dtype.char == "i" and a.flags.c_contiguous:
+        if a.dtype.char == "i" and a.dtype.isnative and a.flags.c_contiguous and a.size == n:
             return C.addressof(C.c_int32.from_buffer(a)), a
-    except (AttributeError, TypeError, ValueError):        # no array, or a read-only or empty one
+    except (AttributeError, TypeError, ValueError):        # no array, or a read-only one
         pass
     import numpy as np
     a = np.ascontiguousarray(a, dtype=np.int32)
+    if a.size != n:
+        raise ValueError(f"{a.size} host counts for {n} traces")
     return a.ctypes.data, a
 
 
@@ -403,7 +405,7 @@ def confspec_op_kv4_append(ctx, kv: KV4, batch: Batch, layer: int, qkv, n_append
                            stream=None) -> None:
     """qkv: fp32 rows of qkv_stride elements (default: the tensor's row stride).  n_append / h_n_append: device tensor and
     host int32 array, or both None (every token)."""
-    hp, keep = (None, None) if h_n_append is None else _host_i32(h_n_append)
+    hp, keep = (None, None) if h_n_append is None else _host_i32(h_n_append, batch.B)
     _check(ctx, lib.confspec_op_kv4_append(ctx, C.byref(kv), C.byref(batch), layer, _ptr(qkv),
                                            qkv.stride(0) if qkv_stride is None else qkv_stride, _ptr(n_append), hp, _ptr(q),
                                            _ptr(k), _ptr(v), _stream_handle(stream)))

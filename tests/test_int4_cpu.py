@@ -127,13 +127,17 @@ def test_cache_operators_refuse_bad_arguments():
 
 def test_host_counts_are_read_where_they_are_or_copied():
     a = np.arange(5, dtype=np.int32)
-    address, keep = cb._host_i32(a)
+    address, keep = cb._host_i32(a, 5)
     assert address == a.ctypes.data and keep is a
     frozen = a.copy()
     frozen.setflags(write=False)
-    for other in (frozen, a[::2], a.astype(np.int64), [0, 1, 2, 3, 4], (7,), a[:0]):
-        address, keep = cb._host_i32(other)
-        assert keep.dtype == np.int32 and keep.flags.c_contiguous and address == keep.ctypes.data and keep.tolist() == list(other)
+    for other in (frozen, np.arange(10, dtype=np.int32)[::2], a.astype(np.int64), a.astype(">i4"), [0, 1, 2, 3, 4], (7,)):
+        address, keep = cb._host_i32(other, len(other))
+        assert keep.dtype == np.int32 and keep.dtype.isnative and keep.flags.c_contiguous and address == keep.ctypes.data
+        assert keep.tolist() == list(other)
+    for short in (a[:4], a[:0], [1, 2, 3, 4], [1] * 6):
+        with pytest.raises(ValueError):
+            cb._host_i32(short, 5)
 
 
 @pytest.mark.parametrize("S, L", [((1,), (100000,)), ((1, 1, 1), (0, 5, 70000)), ((300,), (40000,)), ((7,) * 40, (3000,) * 40)])
