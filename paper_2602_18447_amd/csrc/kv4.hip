@@ -666,11 +666,15 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_
             return table[min(page, kv.max_blocks - 1)];
         };
         int ids = block_ids(0), ids_next = block_ids(32);
-        auto load = [&](Chunk4 &d, int i) {      // (a chunk behind the last one reads zeros, and touches no memory)
+        auto load = [&](Chunk4 &d, int i) {      // called with 0, 1, 2, ... (a chunk behind the last one reads zeros, and touches no memory)
+            if (i && (i & 31) == 0) {
+                ids = ids_next;
+                ids_next = block_ids(i + 32);
+            }
             const unsigned bytes = c_begin + wk + WK * i < c_stop ? KV4_PAGE : 0;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int id = min(max(__builtin_amdgcn_readlane((i & 31) == 0 && i ? ids_next : ids, 2 * (i & 31) + x), 0), kv.n_blocks - 1);
+                const int id = min(max(__builtin_amdgcn_readlane(ids, 2 * (i & 31) + x), 0), kv.n_blocks - 1);
                 const Loads page(head + (size_t)id * block_bytes, bytes);
                 d.k[x] = page.get(at16);
                 d.v[x] = page.get(KV4_V + at16);
@@ -689,10 +693,6 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_
         for (int i = 0; i < n; i += 2) {
             load(c1, i + 1);
             compute(c0, i);
-            if ((i & 31) == 30) {                // the next 32 chunks' numbers are in use from here on
-                ids = ids_next;
-                ids_next = block_ids(i + 34);
-            }
             load(c0, i + 2);
             if (i + 1 < n) compute(c1, i + 1);
         }

@@ -312,6 +312,12 @@ def test_attention_long(L, S):
     _attn_case(6, 1, L, S, 11)
 
 
+@pytest.mark.parametrize("Hq, Hkv, L, S", [(35, 1, (9600,), (128,)), (8, 8, (12000,) * 17, (1,) * 17), (64, 1, (27000,), (150,))])
+def test_attention_wavefronts_with_more_than_32_chunks(Hq, Hkv, L, S):
+    """Batches whose pieces are long: a wavefront's block numbers come in several rounds."""
+    _attn_case(Hq, Hkv, L, S, 19, poison=False)
+
+
 @pytest.mark.parametrize("q_scale", [0.0, 1e-3, 8.0, 60.0])
 def test_attention_from_even_to_single_weights(q_scale):
     _attn_case(4, 2, (700, 33), (3, 1), 12, q_scale=q_scale)
