@@ -65,7 +65,11 @@ __device__ __forceinline__ void sincos64(double x, double &s, double &c) {
 }
 
 // Half a wavefront per head, eight heads a workgroup at a time, n_split workgroups per token; lane i of a half has elements 2 i, 2 i + 1
-// and the 64 further ones they are paired with.  Bound by the bytes of qkv and of q, k, v where tokens are many.
+// and the 64 further ones they are paired with: minimum, maximum and the words of codes need exchanges inside the half only.
+// Rotated: (x, y) -> (x cos - y sin, y cos + x sin), angle (L_b + i) theta^(-j / 64).  Angles and rotation in 64 bits, whose time is
+// hidden while tokens are few; codes in fp32, whose error moves one only where (x - z) / s lies within 2^-20 of a tie.
+// Bound by the bytes of qkv and of q, k, v where tokens are many: 4096 tokens, 40 heads on 8: 33.5 us for 181 MB (5.4 TB/s); by latency
+// (length, block number, row) where they are few: one token 3.3 us, of 12 heads on 2.
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_split) {
     const Kv4Batch &b = a.b;
     const int t = blockIdx.x / n_split, split = blockIdx.x % n_split, lane = threadIdx.x & 63, i2 = lane & 31, heads = a.Hq + 2 * b.Hkv;
@@ -137,7 +141,7 @@ __device__ __forceinline__ float param_s(unsigned p) { return __half2float(__ush
 __device__ __forceinline__ float param_z(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p >> 16))); }
 
 // Eight heads of a token a workgroup, four at a time: a wavefront has a head's key and value row, a thread half a word of it, so that
-// a wavefront's stores are 512 consecutive bytes twice.
+// a wavefront's stores are 512 consecutive bytes twice.  Bound by what it writes: 4096 tokens, 8 heads: 10.9 us for 38 MB (3.5 TB/s).
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, float *__restrict__ k, float *__restrict__ v) {
     const int t = blockIdx.x / n_split, lane = threadIdx.x & 63, h0 = blockIdx.x % n_split * 8 + (threadIdx.x >> 6);
     const int trace = trace_of(b.cu, b.B, t, lane);
@@ -176,7 +180,10 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, 
 //    looks at the halves that come out; only where one has grown too large, M is raised, what was summed scaled and the chunk's
 //    probabilities taken again.
 //
-// Bound by the cache's bytes when rows are few (136 bytes a token and head), by the vector pipe when they are many.
+// Bound by the cache's bytes when rows are few (136 bytes a token and head: 48 traces of 2000 to 16384 tokens, 40 heads on 8: 94 us for
+// 478 MB, 5.1 TB/s, and 5.4 to join the pieces), by the vector pipe when they are many (16 traces of 32 to 256 tokens on 512 to 8192, 12
+// heads on 2: 138 us, 0.54 PFLOP/s; a chunk is 224 vector instructions and 32 products of 32 rows by 32 keys), by latency when the batch
+// is small (one token on 2048: 8.7 us, and 3.5 to join).
 constexpr int ATT_TRACES = 256;       // traces of one launch
 struct AttnPlan4 {
     int32_t b0, nb;                   // traces
@@ -766,7 +773,8 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_
     }
 }
 
-// One wavefront per (head, row) of the traces that were cut: a lane has two columns.
+// One wavefront per (head, row) of the traces that were cut: a lane has two columns.  The sum over pieces of exp2(M_p - M) (O_p, l_p), M the
+// largest of them; bound by its reads of O: 19884 rows of 128 in some 3 pieces 12 us, 1920 in some 5 pieces 5.4 us.
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 plan, int rows_log2, const float *__restrict__ part_o,
                                                         const float2 *__restrict__ part_ml) {
     const Kv4Batch &kv = a.b;

@@ -14,7 +14,8 @@ __device__ __forceinline__ int w4_source_row(int nt, int m, int N, int gate_up) 
     return (m & 8) ? N / 2 + f : f;
 }
 
-// One workgroup per record: 256 words, then the pairs (s, z / 16) of row 0's groups, row 1's, ...  What lies behind K is zero.
+// One workgroup per record: 256 words, then the pairs (s, z / 16) of row 0's groups, row 1's, ...  What lies behind K is zero.  Done once
+// per matrix: N = 55296, K = 5120 (142 MB of codes, 301 MB in all) 149 us.
 __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t *__restrict__ codes, const __half *__restrict__ scales,
                                                       const __half *__restrict__ zeros, uint8_t *__restrict__ dst, int N, int K,
                                                       int group, int gate_up, int record, int n_kb) {
@@ -70,7 +71,10 @@ __device__ __forceinline__ bf16x8 code_operand(unsigned w, CodeBits b) {
 //    -16 everywhere: it takes the offset out, and leaves -16 sum(a) of the group, which z / 16 is multiplied by.
 //  * A lane has one row of W and four rows of A in the result, so that a group costs two multiply-adds a result, which take s and z
 //    as the halves they are: sum += s (part - z sum(a)).
-// Bound by the bytes of W while rows are few; every workgroup reads its rows of A from L2.
+// Bound by the bytes of W while rows are few; every workgroup reads its rows of A from L2.  N = 55296, K = 5120, groups of 128, one row: 24.8
+// us (6.1 TB/s, the weights come from the last-level cache; 30 with other weights each time, 5.0).  N = 5120, K = 27648, groups of 64, 8
+// rows: 19.2 us (4.1 TB/s; 24.2), as its 160 tiles of 32 rows leave 96 CUs without.  72 rows, N = 7168, K = 5120, groups of 32: 22.4 us,
+// bound by the vector pipe (8 multiply-adds a group and 16 x 16 results, 128 to unpack 64 x 128 codes) and its turns with the matrix pipe.
 template <int NG>
 struct Params;
 template <> struct Params<1> { typedef unsigned T; static __device__ unsigned get(T p, int) { return p; } };

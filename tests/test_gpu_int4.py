@@ -307,7 +307,7 @@ def test_attention_many_rows_on_few_keys(Hq, Hkv, L, S):
     _attn_case(Hq, Hkv, L, S, 18)
 
 
-@pytest.mark.parametrize("L, S", [((40000,), (1,)), ((20000, 5), (2, 3)), ((9000,), (150,)), ((0, 10), (400, 300))])
+@pytest.mark.parametrize("L, S", [((40000,), (1,)), ((150000, 70000), (1, 5)), ((20000, 5), (2, 3)), ((9000,), (150,)), ((0, 10), (400, 300))])
 def test_attention_long(L, S):
     _attn_case(6, 1, L, S, 11)
 
