@@ -66,8 +66,8 @@ __device__ __forceinline__ void sincos64(double x, double &s, double &c) {
 
 // Half a wavefront per head, eight heads a workgroup at a time, n_split workgroups per token; lane i of a half has elements 2 i, 2 i + 1
 // and the 64 further ones they are paired with: minimum, maximum and the words of codes need exchanges inside the half only.
-// Rotated: (x, y) -> (x cos - y sin, y cos + x sin), angle (L_b + i) theta^(-j / 64).  Angles and rotation in 64 bits, whose time is
-// hidden while tokens are few; codes in fp32, whose error moves one only where (x - z) / s lies within 2^-20 of a tie.
+// Rotated: (x, y) -> (x cos - y sin, y cos + x sin), angle (L_b + i) theta^(-j / 64).  Angles, rotation and what decides between
+// two codes in 64 bits.
 // Bound by the bytes of qkv and of q, k, v where tokens are many: 4096 tokens, 40 heads on 8: 33.5 us for 181 MB (5.4 TB/s); by latency
 // (length, block number, row) where they are few: one token 3.3 us, of 12 heads on 2.
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_split) {
@@ -116,9 +116,25 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
             const float z = __half2float(zh);
             const __half sh = __float2half_rn((float)(((double)mx - (double)z) / 15.0) + 0.f);
             const float s = __half2float(sh);
+            float n[4];
+            bool close = false;                                     // a quotient that is a tie within its error, 16 times a few 2^-24
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float quotient = (x[e] - z) / s;
+                n[e] = rintf(quotient);
+                close |= fabsf(fabsf(quotient - n[e]) - 0.5f) < 0x1p-17f;
+            }
+            if (__any(close))                                       // what is left of the element decides, in 64 bits
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const double left = fma(-(double)n[e], (double)s, (double)x[e] - (double)z), half = 0.5 * (double)s;
+                    const bool odd = ((int)n[e] & 1) != 0;
+                    if (left > half || (odd && left == half)) n[e] += 1.f;
+                    else if (left < -half || (odd && left == -half)) n[e] -= 1.f;
+                }
             unsigned c[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) c[e] = s > 0.f ? (unsigned)fminf(fmaxf(rintf((x[e] - z) / s), 0.f), 15.f) : 0u;
+            for (int e = 0; e < 4; ++e) c[e] = s > 0.f ? (unsigned)fminf(fmaxf(n[e], 0.f), 15.f) : 0u;
             const int e = 2 * (lane & 3);                           // place of the first of the lane's two in their word of eight
             unsigned w0 = is_k ? c[0] << k_shift(e) | c[1] << k_shift(e + 1) : (c[0] | c[1] << 4) << (4 * e);
             unsigned w1 = is_k ? c[2] << k_shift(e) | c[3] << k_shift(e + 1) : (c[2] | c[3] << 4) << (4 * e);

@@ -230,6 +230,19 @@ def test_append_at_far_positions(theta):
     _append_case(2, 1, (200000, 131071), (3, 18), None, 79, theta=theta)
 
 
+def test_append_elements_next_to_a_tie():
+    """Rows from 2^-k to a half's largest values, whose elements lie near (c + 1/2) s: codes as the exact quotient has them."""
+    def edit(x, Hq, Hkv):
+        gen = _gen(45)
+        n = x.shape[0] * Hkv
+        lo = -(2.0 ** torch.randint(-14, 4, (n, 1), generator=gen, device=DEV)) * (1 + torch.randint(0, 128, (n, 1), generator=gen, device=DEV) / 128.0)
+        hi = 2.0 ** torch.randint(-8, 12, (n, 1), generator=gen, device=DEV) * (1 + torch.randint(0, 128, (n, 1), generator=gen, device=DEV) / 128.0)
+        v = lo + (hi - lo) * (torch.randint(0, 15, (n, 128), generator=gen, device=DEV) + 0.5) / 15.0
+        v[:, :1], v[:, 1:2] = lo, hi
+        x[:, Hq + Hkv:] = v.view(-1, Hkv, 128)
+    _append_case(4, 4, (9, 0), (150, 90), None, 46, edit=edit)
+
+
 def test_append_rows_of_every_kind():
     _append_case(3, 3, (13,), (12,), None, 80, edit=_edit_values)
 
