@@ -849,7 +849,7 @@ struct Launch4 {
 };
 // Pieces are of 32 chunks at least.  With eight wavefronts one workgroup fits a CU, and what does not fit at once waits for a whole item: as
 // few items as there are CUs (one token on 16384 keys, 12 heads on 2: 13.7 us; in pieces of a power of two of chunks, which leave some CUs
-// without, 18).  With four, two or three fit, and more items even out (16 traces of 32 to 256 tokens: 141 us, with 1024 items 147).
+// without, 18).  With four, two or three fit, and more items even out (16 traces of 32 to 256 tokens: 135 us, with 1024 items 141).
 constexpr int ATT_MIN_CHUNKS = 32;
 constexpr int att_slots(int wk) { return wk == 8 ? 256 : 1536; }
 

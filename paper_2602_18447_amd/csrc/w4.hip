@@ -270,8 +270,8 @@ hipError_t launch_w4_pack(const uint8_t *codes, const __half *scales, const __ha
 }
 
 // Which rows of A and of W a workgroup takes, and how many wavefronts share its k.  Up to 16 rows the bytes of W bound the product:
-// 32 rows of W a workgroup once there are 256 tiles of 16 (N = 5120, K = 27648, 8 rows, groups of 64: 24 us, with 16 rows of W 29;
-// N = 1536, K = 8960, one row: 7.6, with 16 rows 5.6), wavefronts to about 2048 in all, each with at least one and a half blocks.
+// 32 rows of W a workgroup once there are 256 tiles of 16 (N = 5120, K = 27648, 8 rows, groups of 64: 24.2 us, with 16 rows of W 29.9;
+// N = 1536, K = 8960, one row: 7.2, with 16 rows 5.5), wavefronts to about 2048 in all, each with at least one and a half blocks.
 // More rows are bound by the vector and matrix pipes: the tile with the least of w4_cost, in rounds of 256 workgroups.  Measured (us)
 // for 2x2, 2x4, 3x2, 3x4, 4x4 tiles of 16: 72 rows, N = 7168, K = 5120, groups of 128: 21.0, 19.9, 19.8, 16.2, 19.8;  48, 5120, 5120, 64:
 // 15.6, 14.4, 13.8, 17.9, -;  128, 1536, 8960, 128: 14.7, 18.3, 17.3, -, -;  128, 55296, 5120, 128: 166, 131, -, 139, 120.
