@@ -12,8 +12,8 @@
  * Same conventions as confspec.h: dev pointers are caller-owned device memory, nothing is allocated, nothing
  * synchronises, every check that host-visible arguments allow is made before the first launch.  The calls can be
  * captured into HIP graphs; calls on different streams may run at the same time as long as their outputs, scratch
- * and written cache rows differ.  All of them need a bf16 context (head_dim 128); other contexts get
- * CONFSPEC_E_UNSUPPORTED.
+ * and written cache rows differ.  Outputs overlap no other operand unless a function says so.  All of them need a bf16
+ * context (head_dim 128); other contexts get CONFSPEC_E_UNSUPPORTED.
  */
 #ifndef CONFSPEC_INT4_H
 #define CONFSPEC_INT4_H

@@ -68,8 +68,9 @@ __device__ __forceinline__ void sincos64(double x, double &s, double &c) {
 // and the 64 further ones they are paired with: minimum, maximum and the words of codes need exchanges inside the half only.
 // Rotated: (x, y) -> (x cos - y sin, y cos + x sin), angle (L_b + i) theta^(-j / 64).  Angles, rotation and what decides between
 // two codes in 64 bits.
-// Bound by the bytes of qkv and of q, k, v where tokens are many: 4096 tokens, 40 heads on 8: 33.5 us for 181 MB (5.4 TB/s); by latency
-// (length, block number, row) where they are few: one token 3.3 us, of 12 heads on 2.
+// Bound by the bytes of qkv and of q, k, v where tokens are many: 4096 tokens, 40 heads on 8: 34 us for 181 MB (5.3 TB/s); by latency
+// (length, block number, row) where they are few: one token 3.7 us, of 12 heads on 2.  A wavefront's 64 lanes take the token's 64 angles for
+// all (2362 tokens, 12 heads on 2: 9.8 us; each half its own, 10.9).
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_split) {
     const Kv4Batch &b = a.b;
     const int t = blockIdx.x / n_split, split = blockIdx.x % n_split, lane = threadIdx.x & 63, i2 = lane & 31, heads = a.Hq + 2 * b.Hkv;
@@ -80,13 +81,17 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
     const int i = min(max(t - b.cu[trace], 0), b.T - 1), row = min(max(b.plens[trace], 0), b.max_L) + i, slot = row & 15;
     const bool store = (!a.n_append || i < a.n_append[trace]) && row >> 4 < b.max_blocks;
     uint8_t *const pages = page_of(b, trace, row, 0);
-    // theta^(-j / 64) for j = 2 i and 2 i + 1, from the six powers theta^(-2^k / 64)
-    double f0 = i2 & 1 ? a.theta_pow[1] : 1.0;
+    // the token's 64 angles, once: theta^(-j / 64) from the six powers theta^(-2^k / 64)
+    __shared__ double2 s_turn[64];
+    if (threadIdx.x < 64) {
+        double f = 1.0, sn, cs;
 #pragma unroll
-    for (int k = 1; k < 5; ++k) f0 *= (i2 >> k) & 1 ? a.theta_pow[k + 1] : 1.0;
-    double s0, c0, s1, c1;
-    sincos64((double)row * f0, s0, c0);
-    sincos64((double)row * (f0 * a.theta_pow[0]), s1, c1);
+        for (int k = 0; k < 6; ++k) f *= (lane >> k) & 1 ? a.theta_pow[k] : 1.0;
+        sincos64((double)row * f, sn, cs);
+        s_turn[lane] = make_double2(cs, sn);
+    }
+    __syncthreads();
+    const double c0 = s_turn[2 * i2].x, s0 = s_turn[2 * i2].y, c1 = s_turn[2 * i2 + 1].x, s1 = s_turn[2 * i2 + 1].y;
     for (; h < heads; h += 8 * n_split) {
         float2 lo_next = lo, hi_next = hi;
         if (h + 8 * n_split < heads) {
