@@ -316,7 +316,7 @@ __device__ __forceinline__ void probabilities(f16x8 &w, float &l, float &zs, flo
 
 // 32 cached tokens, of which the first n_valid count; what is stored for the others may be anything.
 template <int NQ>
-__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g, bool &big) {
+__device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int n_valid, int g, bool first, bool &big) {
     f32x4 sc[NQ][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -346,8 +346,8 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
     // With the references as they are, unless that was too much for a half or an addend of the sums; most chunks end here.
     f16x8 w[NQ];
     float l[NQ], zs[NQ];
-    bool over = big;
-    if (!big) {
+    bool over = big || first;         // (there is no reference before the first)
+    if (!over) {
         f16x2 top = {0, 0};
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -712,7 +712,7 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_
             __builtin_amdgcn_sched_barrier(0);   // (loads stay ahead of the products before them in time)
         };
         auto compute = [&](const Chunk4 &d, int i) {
-            cached_chunk<NQ>(R, d, L - 32 * (c_begin + wk + WK * i), g, big);
+            cached_chunk<NQ>(R, d, L - 32 * (c_begin + wk + WK * i), g, i == 0, big);
             __builtin_amdgcn_sched_barrier(0);
         };
         const int n = (c_stop - c_begin - wk + WK - 1) / WK;
