@@ -73,7 +73,7 @@ __device__ __forceinline__ bf16x8 code_operand(unsigned w, CodeBits b) {
 //    as the halves they are: sum += s (part - z sum(a)).
 // Bound by the bytes of W while rows are few; every workgroup reads its rows of A from L2.  N = 55296, K = 5120, groups of 128, one row: 24.8
 // us (6.1 TB/s, the weights come from the last-level cache; 30 with other weights each time, 5.0).  N = 5120, K = 27648, groups of 64, 8
-// rows: 19.2 us (4.1 TB/s; 24.2), as its 160 tiles of 32 rows leave 96 CUs without.  72 rows, N = 7168, K = 5120, groups of 32: 22.4 us,
+// rows: 19.2 us (4.2 TB/s; 24.2), as its 160 tiles of 32 rows leave 96 CUs without.  72 rows, N = 7168, K = 5120, groups of 32: 22.4 us,
 // bound by the vector pipe (8 multiply-adds a group and 16 x 16 results, 128 to unpack 64 x 128 codes) and its turns with the matrix pipe.
 template <int NG>
 struct Params;
@@ -271,8 +271,14 @@ hipError_t launch_w4_pack(const uint8_t *codes, const __half *scales, const __ha
 
 // Which rows of A and of W a workgroup takes, and how many wavefronts share its k.  Up to 16 rows the bytes of W bound the product:
 // 32 rows of W a workgroup once there are 256 tiles of 16 (N = 5120, K = 27648, 8 rows, groups of 64: 24.2 us, with 16 rows of W 29.9;
-// N = 1536, K = 8960, one row: 7.2, with 16 rows 5.5), wavefronts to about 2048 in all, each with at least one and a half blocks.
-// More rows are bound by the vector and matrix pipes: the tile with the least of w4_cost, in rounds of 256 workgroups.  Measured (us)
+// N = 1536, K = 8960, one row: 7.2, with 16 rows 5.5), 4 wavefronts from 512 workgroups on (N = 55296, K = 5120, one row: 29.6, 8 32.8), 8 from
+// 256, else 16 (160 workgroups, the first of these: 19.2, 8 21.8 on weights read just before; 24.2, 22.8 on others), if there are as many
+// blocks of k (N = 5120, K = 1408, 4 rows: 8 wavefronts 4.2, 11 4.4).
+// More rows on a small matrix are bound by what a workgroup can fetch, and tiles of 1 x 1 or 1 x 2 make the most workgroups, up to one a CU.
+// Measured (us) for 1x1, 1x2 and 2x2 with 8 wavefronts, at so many tiles of 16 x 16: 34 (25 rows, N = 272, K = 17824, groups of 32): 12.7,
+// 17.1, 28.3;  256 (20, 2048, 4096, 128): 5.5, 6.0, 8.0;  288 (40, 1536, 4096, 64): 7.8, 6.4, 8.2;  512 (20, 4096, 2048, 64): 6.0, 5.3, 6.0;
+// 640 (30, 5120, 5120, 128): 16.7, 12.3, 10.9;  768 (128, 1536, 8960, 128): 21.5, 17.3, 14.9.
+// Others are bound by the vector and matrix pipes: the tile with the least of w4_cost, in rounds of 256 workgroups.  Measured (us)
 // for 2x2, 2x4, 3x2, 3x4, 4x4 tiles of 16: 72 rows, N = 7168, K = 5120, groups of 128: 21.0, 19.9, 19.8, 16.2, 19.8;  48, 5120, 5120, 64:
 // 15.6, 14.4, 13.8, 17.9, -;  128, 1536, 8960, 128: 14.7, 18.3, 17.3, -, -;  128, 55296, 5120, 128: 166, 131, -, 139, 120.
 struct W4Tile { int mt, nt, W; };
@@ -283,13 +289,13 @@ int w4_cost(int mt, int nt, int ng) {    // issue cycles of a wavefront's block,
 
 W4Tile w4_tile(int M, int N, int K, int group) {
     const int tiles = N / 16, n_kb = w4_kblocks(K);
-    W4Tile t = {1, 1, 4};
-    long groups;
+    const long small = (long)((M + 15) / 16) * tiles;
+    W4Tile t = {1, small <= 256 ? 1 : 2, 8};
     if (M <= 16) {
         t.nt = tiles >= 256 ? 2 : 1;
-        groups = (tiles + t.nt - 1) / t.nt;
-        while (t.W < 16 && groups * t.W < 2048) t.W *= 2;
-    } else {
+        const long groups = (tiles + t.nt - 1) / t.nt;
+        t.W = groups >= 512 ? 4 : groups >= 256 || n_kb < 16 ? 8 : 16;
+    } else if (small > 512) {
         long best = -1;
         for (const auto &c : {W4Tile{2, 2, 0}, W4Tile{2, 4, 0}, W4Tile{3, 2, 0}, W4Tile{3, 4, 0}, W4Tile{4, 4, 0}}) {
             const long units = (long)((M + 16 * c.mt - 1) / (16 * c.mt)) * ((tiles + c.nt - 1) / c.nt);
@@ -301,7 +307,6 @@ W4Tile w4_tile(int M, int N, int K, int group) {
             }
         }
     }
-    while (t.W > 4 && 2 * n_kb < 3 * t.W) t.W /= 2;
     t.W = std::min(t.W, n_kb);
     return t;
 }

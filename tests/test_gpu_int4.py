@@ -124,6 +124,13 @@ def test_w4_shapes(N, K, group, M, epi):
     _w4_case(M, N, K, group, epi, N + K + M)
 
 
+@pytest.mark.parametrize("M, N", [(20, 5136), (32, 4112), (17, 8208), (64, 10256), (40, 4144), (33, 8208), (90, 7200), (100, 6160), (128, 12304), (70, 2576), (33, 2320)])
+@pytest.mark.parametrize("K, group, epi", [(416, 32, 0), (1088, 64, 1), (640, 128, 2)])
+def test_w4_many_rows_on_wide_matrices(M, N, K, group, epi):
+    """Every tile that more than 16 rows can take."""
+    _w4_case(M, N, K, group, epi, 9)
+
+
 @pytest.mark.parametrize("M", [1, 40])
 def test_w4_zero_points_of_eight_when_none_are_given(M):
     _w4_case(M, 272, 640, 128, cb.EPI_STORE_F32, 5, zeros=False)
