@@ -29,7 +29,8 @@ extern "C" {
  * two IEEE halves s and z.  A row x (bf16 values, clamped to +-65504) is stored as
  *     z = half(min x),  s = half(fp32((max x - z) / 15)),  c = (x - z) / s to the nearest whole number, ties to even,
  *     within 0..15 (0 where s is 0); a zero s or z is +0.
- * A NaN among the elements is stored as some number of the row's range.
+ * A row with a NaN among its elements stands for NaN throughout: s and z are 0x7E00, codes 0 (its finite elements are lost, and
+ * the attention of the rows that see it is NaN, as it is with a NaN among bf16 keys or values).
  * Keys are stored rotated.  A page holds 16 tokens of one head, keys and values:
  *   byte    0  key codes: 32-bit word ((c * 16 + token) * 4 + i) has elements d = 32 i + 8 c + e, e = 0..7, the even
  *              e in bits 2 e .. 2 e + 3 and the odd ones in bits 2 e + 14 .. 2 e + 17

@@ -113,7 +113,12 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
             // min and max of the row, its pair (s, z), the codes
             float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_fmed3f(bf16_f32(r[e]), -65504.f, 65504.f);
+            for (int e = 0; e < 4; ++e) x[e] = bf16_f32(r[e]);
+            // A NaN anywhere in the row: s and z are NaN, which is what the definition's minimum is (v_med3 below would take it for -65504).
+            const unsigned long long nan_lanes = __ballot(__builtin_isunordered(x[0], x[1]) || __builtin_isunordered(x[2], x[3]));
+            const bool nan = (unsigned)(nan_lanes >> (lane & 32)) != 0u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_fmed3f(x[e], -65504.f, 65504.f);
             float mn = fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) { mn = fminf(mn, __shfl_xor(mn, o, 64)); mx = fmaxf(mx, __shfl_xor(mx, o, 64)); }
@@ -139,7 +144,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
                 }
             unsigned c[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) c[e] = s > 0.f ? (unsigned)fminf(fmaxf(n[e], 0.f), 15.f) : 0u;
+            for (int e = 0; e < 4; ++e) c[e] = s > 0.f && !nan ? (unsigned)fminf(fmaxf(n[e], 0.f), 15.f) : 0u;
             const int e = 2 * (lane & 3);                           // place of the first of the lane's two in their word of eight
             unsigned w0 = is_k ? c[0] << k_shift(e) | c[1] << k_shift(e + 1) : (c[0] | c[1] << 4) << (4 * e);
             unsigned w1 = is_k ? c[2] << k_shift(e) | c[3] << k_shift(e + 1) : (c[2] | c[3] << 4) << (4 * e);
@@ -151,7 +156,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
                 *(unsigned *)(page + (is_k ? k_word(slot, 2 * i2 + 64) : v_word(slot, 2 * i2 + 64))) = w1;
             }
             if (i2 == 0)
-                *(unsigned *)(page + (is_k ? KV4_KP : KV4_VP) + slot * 4) = (unsigned)__half_as_ushort(sh) | (unsigned)__half_as_ushort(zh) << 16;
+                *(unsigned *)(page + (is_k ? KV4_KP : KV4_VP) + slot * 4) =
+                    nan ? 0x7E007E00u : (unsigned)__half_as_ushort(sh) | (unsigned)__half_as_ushort(zh) << 16;
         }
         lo = lo_next;
         hi = hi_next;
