@@ -64,6 +64,13 @@ __device__ __forceinline__ void sincos64(double x, double &s, double &c) {
     c = (quadrant == 1 || quadrant == 2) ? -b : b;
 }
 
+// x as a half, a zero without its sign: 0 is added after the rounding, as all from -2^-25 on rounds to -0.  (The compiler may not see
+// where x comes from: of a rounding from 64 bits to fp32 and this one it would make one.)
+__device__ __forceinline__ __half half_unsigned_zero(float x) {
+    asm("" : "+v"(x));
+    return __builtin_bit_cast(__half, (_Float16)((_Float16)x + (_Float16)0.f));
+}
+
 // Half a wavefront per head, eight heads a workgroup at a time, n_split workgroups per token; lane i of a half has elements 2 i, 2 i + 1
 // and the 64 further ones they are paired with: minimum, maximum and the words of codes need exchanges inside the half only.
 // Rotated: (x, y) -> (x cos - y sin, y cos + x sin), angle (L_b + i) theta^(-j / 64).  Angles, rotation and what decides between
@@ -122,9 +129,9 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
             float mn = fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) { mn = fminf(mn, __shfl_xor(mn, o, 64)); mx = fmaxf(mx, __shfl_xor(mx, o, 64)); }
-            const __half zh = __float2half_rn(mn + 0.f);            // (never -0)
+            const __half zh = half_unsigned_zero(mn);
             const float z = __half2float(zh);
-            const __half sh = __float2half_rn((float)(((double)mx - (double)z) / 15.0) + 0.f);
+            const __half sh = half_unsigned_zero((float)(((double)mx - (double)z) / 15.0));
             const float s = __half2float(sh);
             float n[4];
             bool close = false;                                     // a quotient that is a tie within its error, 16 times a few 2^-24

@@ -6,7 +6,7 @@ import torch
 
 from paper_2602_18447_amd import binding as cb
 from tests import int4_ref as R
-from tests.test_gpu_int4 import DEV, Cache, Ctx, _attn_check, _gen
+from tests.test_gpu_int4 import DEV, Cache, Ctx, _append_case, _attn_check, _gen
 
 pytestmark = pytest.mark.gpu
 NAN_HALF = torch.tensor([0x7E00], dtype=torch.int16).view(torch.float16)[0]
@@ -74,3 +74,21 @@ def test_attention_over_a_row_stored_as_nan(L, S, is_v):
     seen = torch.zeros(c.T, Hq, dtype=torch.bool, device=DEV)
     seen[:S[0], 15:20] = True
     assert bool(torch.isnan(out[seen]).all()) and torch.equal(out[~seen], good[~seen])
+
+
+def test_append_a_zero_has_no_sign():
+    """Rows whose minimum or range rounds to a zero half from below: bytes as the plain form has them."""
+    def edit(x, Hq, Hkv):
+        for rows in (x[:, Hq + Hkv:], x[:1, Hq:Hq + Hkv]):             # (keys at position 0 are not turned)
+            for t in range(rows.shape[0]):
+                rows[t] = torch.rand(Hkv, 128, generator=_gen(t), device=DEV) * 1e-3
+        v = x[:, Hq + Hkv:]
+        v[0, :, 3] = -1e-9                                             # z from (-2^-25, 0)
+        v[1, :, 100] = -2.0 ** -26
+        v[2] = 1.5 * 2.0 ** -25                                        # z is 2^-24, beyond the maximum: s from below 0
+        v[3] = -2.0 ** -26
+        v[4] = -0.0
+        v[5] = -1e-9
+        v[5, :, 9] = 1e-9
+        x[0, Hq:Hq + Hkv, 70] = -1e-9
+    _append_case(3, 3, (0,), (6,), None, 52, edit=edit)
