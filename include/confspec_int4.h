@@ -104,7 +104,8 @@ int confspec_w4_pack(confspec_ctx *ctx, const void *dev_codes, const void *dev_s
  *   CONFSPEC_EPI_SWIGLU    : W packed with gate_up = 1; out bf16 [M, N / 2] = silu(gate) * up
  * dev_residual is read by the residual epilogue only and must be NULL otherwise.  Operands are 16-byte aligned.
  * Products of codes and activations are exact, their sums within a group and over the groups fp32, added in an order
- * that only the shape decides. */
+ * that only the shape decides.  A result that is no finite number so (infinite activations; sums of 31 times the activations beyond
+ * fp32) is what the sum of activations times weights is, taken in fp32 group by group. */
 int confspec_op_w4_gemm(confspec_ctx *ctx, const void *dev_A, const void *dev_W4, const float *dev_residual, void *dev_out,
                         int32_t M, int32_t N, int32_t K, int32_t group, int32_t epilogue, confspec_stream stream);
 

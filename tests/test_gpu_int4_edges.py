@@ -6,7 +6,7 @@ import torch
 
 from paper_2602_18447_amd import binding as cb
 from tests import int4_ref as R
-from tests.test_gpu_int4 import DEV, Cache, Ctx, _append_case, _attn_check, _gen
+from tests.test_gpu_int4 import DEV, Cache, Ctx, _append_case, _attn_check, _gen, _w4_case
 
 pytestmark = pytest.mark.gpu
 NAN_HALF = torch.tensor([0x7E00], dtype=torch.int16).view(torch.float16)[0]
@@ -92,3 +92,50 @@ def test_append_a_zero_has_no_sign():
         v[5, :, 9] = 1e-9
         x[0, Hq:Hq + Hkv, 70] = -1e-9
     _append_case(3, 3, (0,), (6,), None, 52, edit=edit)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# products
+# ---------------------------------------------------------------------------------------------------------------------
+W4_TILES = [(1, 48, 416, 32, 0), (4, 5136, 416, 32, 1), (7, 144, 1600, 64, 1), (16, 4112, 640, 128, 0), (12, 32, 160, 32, 2), (20, 272, 1088, 64, 0), (40, 2576, 640, 128, 1),
+            (17, 8208, 416, 32, 0), (32, 4112, 1088, 64, 2), (48, 7200, 640, 128, 0), (70, 12304, 416, 32, 1), (100, 6160, 1088, 64, 0), (128, 12304, 640, 128, 0)]
+
+
+@pytest.mark.parametrize("M, N, K, group, epi", W4_TILES)
+def test_w4_infinite_activations(M, N, K, group, epi):
+    """An infinity times a weight that is not 0 is an infinity: what the definition has, element by element."""
+    gen = _gen(53)
+    codes, s, z, w = R.w4_quantise_case(gen, N, K, group, DEV)
+    a = torch.randn(M, K, generator=gen, device=DEV).bfloat16()
+    inf = float("inf")
+    a[0, 5] = inf
+    if M > 3:
+        a[1, K - 1], a[2, 9], a[2, K - 20], a[3, 33] = -inf, inf, inf, float("nan")
+    if M > 16:
+        a[16, K // 2] = -inf
+    resid = torch.randn(M, N, generator=gen, device=DEV) if epi == cb.EPI_RESID_F32 else None
+    packed = torch.empty(cb.confspec_w4_bytes(N, K, group), dtype=torch.uint8, device=DEV)
+    out = torch.empty(M, N // 2, dtype=torch.bfloat16, device=DEV) if epi == cb.EPI_SWIGLU else torch.empty(M, N, device=DEV)
+    with Ctx() as ctx:
+        cb.confspec_w4_pack(ctx, codes, s, z, N, K, group, packed, gate_up=epi == cb.EPI_SWIGLU)
+        cb.confspec_op_w4_gemm(ctx, a, packed, resid, out, M, N, K, group, epi)
+    zero = torch.zeros_like(a)
+    fin = torch.isfinite(a)
+    y, tol = R.w4_gemm(torch.where(fin, a, zero), w, s, z, group)
+    for m, k in torch.nonzero(~fin).tolist():
+        y[m] += a[m, k].double() * w[:, k]                             # (an infinity, or NaN where the weight is 0)
+    if epi == cb.EPI_SWIGLU:
+        y, tol = R.swiglu(y, tol)
+    elif epi == cb.EPI_RESID_F32:
+        y = y + resid.double()
+        tol = tol + 2.0 ** -24 * y.abs()
+    got, fin = out.double(), torch.isfinite(y)
+    assert not bool(fin[0].any()) and bool(torch.isinf(y[0]).any())
+    assert bool(((got - y).abs() <= tol)[fin].all())
+    assert torch.equal(torch.isnan(got), torch.isnan(y)) and torch.equal(got[torch.isinf(y)], y[torch.isinf(y)])
+
+
+@pytest.mark.parametrize("M, N, K, group, epi", [c for c in W4_TILES if c[4] != 2])
+def test_w4_activations_near_the_largest(M, N, K, group, epi):
+    """31 times an activation and its sums pass the range of fp32, the result does not."""
+    _w4_case(M, N, K, group, epi, 54, scale_a=1e37)
