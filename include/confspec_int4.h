@@ -74,7 +74,9 @@ int confspec_op_kv4_read(confspec_ctx *ctx, const confspec_kv4 *kv, const confsp
  *                  where the need is 0)
  * Numerics: q (below 2^116 in magnitude; taken as halves times a power of two of its row) and codes enter the score product
  * exactly; scores, softmax statistics and sums are fp32; probabilities times the value row's s are rounded to IEEE half for
- * the cached rows, carried as two bf16 terms for the suffix. */
+ * the cached rows, carried as two bf16 terms for the suffix.  Suffix values are below 2^90 in magnitude, or no finite numbers: a weight
+ * is positive, so that an infinity makes its column infinite, and a NaN or infinities of both signs NaN, in the rows that see the
+ * token, and in no other. */
 int confspec_op_kv4_attention(confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_batch *batch, int32_t layer,
                               const void *dev_q, const void *dev_k_suffix, const void *dev_v_suffix, void *dev_out,
                               void *dev_scratch, size_t scratch_bytes, confspec_stream stream);

@@ -294,12 +294,16 @@ struct Rows4 {                        // state of a wavefront's rows: a lane has
     f32x4 o[NQ][8];                   // [j][r]: column 32 (lane / 16) + 8 r + j
 };
 
+// 2^x, x <= 0, never 0: what a sum is scaled by where the reference moves up.  A weight is positive however small, and takes an infinity
+// along; numbers times 2^-126 are lost beside those that raised the reference.
+__device__ __forceinline__ float scale_down(float x) { return fmaxf(__builtin_amdgcn_exp2f(x), 0x1p-126f); }
+
 // Raises the references to the rows' largest score + exponent (t_max: the lane's).
 template <int NQ>
 __device__ __forceinline__ void raise(Rows4<NQ> &R, const float (&t_max)[NQ]) {
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        const float m = fmaxf(R.m[i], max_over_g(t_max[i])), f = __builtin_amdgcn_exp2f(R.m[i] - m);
+        const float m = fmaxf(R.m[i], max_over_g(t_max[i])), f = scale_down(R.m[i] - m);
         R.m[i] = m;
         R.l[i] *= f;
         R.zs[i] *= f;
@@ -428,7 +432,7 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
     }
 }
 
-// Adds the values that attend_suffix takes out of tokens j_begin .. j_end - 1 to the rows that see them.  A probability is positive,
+// Adds the values of tokens j_begin .. j_end - 1 that are not finite numbers to the rows that see them.  A probability is positive,
 // so that an infinity or NaN is what its column becomes, whatever the probability.
 template <int NQ>
 __device__ __forceinline__ void add_not_finite(Rows4<NQ> &R, const bf16 *v, unsigned stride, int j_begin, int j_end, const int (&tok)[NQ], int g) {
@@ -449,6 +453,23 @@ __device__ __forceinline__ void add_not_finite(Rows4<NQ> &R, const bf16 *v, unsi
     }
 }
 
+// Columns that came out as NaN, from the values of the tokens that were attended to: the two terms of a probability may have both
+// signs or be 0, so that an infinity ends as NaN where the definition has an infinity.  (A NaN of the scores or of the cache is in R.l or
+// R.zs too, and stays.)
+template <int NQ>
+__device__ __forceinline__ void settle_not_finite(Rows4<NQ> &R, const bf16 *v, unsigned stride, int j0, int j_step, int j_end, int S, const int (&tok)[NQ], int g) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) R.o[n][j][r] = R.o[n][j][r] == R.o[n][j][r] ? R.o[n][j][r] : 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll 1
+    for (; j0 < j_end; j0 += j_step) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
+}
+
 // Suffix tokens, 32 from j0 on, then from j0 + j_step, below j_end; k, v point at the trace's first token and the head, rows are `stride`
 // elements apart; a row sees tokens up to its own (tok).  Products in bfloat16, probabilities in two terms; R.o is in units of 1.
 // Values are asked for before the scores are taken, the next keys as soon as the registers of these are free.
@@ -456,6 +477,8 @@ template <int NQ>
 __device__ __forceinline__ void attend_suffix(Rows4<NQ> &R, bool &big, const bf16 *q, const int (&q_row)[NQ], const bf16 *k, const bf16 *v, unsigned stride,
                                               int j0, int j_step, int j_end, int S, const int (&tok)[NQ], int n15, int g) {
     bf16x8 qb[NQ][4], kb[2][4];
+    const int j_first = j0;
+    bool whole = false;               // a chunk's values went into the products as they are
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -488,7 +511,9 @@ __device__ __forceinline__ void attend_suffix(Rows4<NQ> &R, bool &big, const bf1
         bool masked = false, bad = false;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) masked |= j0 + 31 > tok[n];
-        if (__any(masked)) {
+        if (!__any(masked)) {
+            whole = true;
+        } else {
             unsigned any = 0;
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
@@ -576,6 +601,16 @@ __device__ __forceinline__ void attend_suffix(Rows4<NQ> &R, bool &big, const bf1
             }
         }
         if (bad) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
+    }
+    if (whole) {
+        float all = 0.f;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) all += R.o[n][j][r];
+        if (__any(all != all)) settle_not_finite<NQ>(R, v, stride, j_first, j_step, j_end, S, tok, g);
     }
 }
 
@@ -796,7 +831,7 @@ __global__ __launch_bounds__(WR * WK * 64, NQ == 1 && WK == 4 ? 3 : 2) void kv4_
 #pragma unroll
             for (int w = 0; w < WK; ++w) {
                 const float2 ml = s_ml[w * ROWS + tile_row];
-                const float f = __builtin_amdgcn_exp2f(ml.x - m);
+                const float f = scale_down(ml.x - m);
                 l += f * ml.y;
                 const float *src = s_o + (w * ROWS + tile_row) * O_PAD + col;
 #pragma unroll
@@ -833,7 +868,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Attn a, AttnPlan4 pla
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
         top = fmaxf(top, m);
-        const float keep = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+        const float keep = scale_down(m - top), f = scale_down(ml.x - top);
         float sum = f * ml.y;
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);

@@ -139,3 +139,49 @@ def test_w4_infinite_activations(M, N, K, group, epi):
 def test_w4_activations_near_the_largest(M, N, K, group, epi):
     """31 times an activation and its sums pass the range of fp32, the result does not."""
     _w4_case(M, N, K, group, epi, 54, scale_a=1e37)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("Hq, Hkv, L, S", [(4, 2, (50, 3), (100, 2)), (12, 2, (5003,), (70,)), (40, 8, (20,) * 6, (100,) * 6), (4, 4, (0,), (300,)), (8, 1, (0, 33), (1, 33)),
+                                           (40, 8, (0,) * 4, (200,) * 4)])
+@pytest.mark.parametrize("weights", ["even", "first_alone", "context_alone"])
+def test_attention_infinite_values_of_tokens_seen(Hq, Hkv, L, S, weights):
+    """A weight is positive, so a column with an infinity is that infinity, with both of them or a NaN it is NaN: in every row that
+    sees the token, however many tokens later and however small the weight is in fp32."""
+    gen = _gen(55)
+    c = Cache(gen, Hkv, L, S)
+    q = torch.randn(c.T, Hq, 128, generator=gen, device=DEV)
+    k = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV)
+    v = torch.randn(c.T, Hkv, 128, generator=gen, device=DEV).bfloat16()
+    last = Hkv - 1
+    n = S[0]
+    bad = [(0, 5, float("inf")), (0, 77, -float("inf")), (n // 3, 40, float("inf")), (n // 2, 41, -float("inf")), (n - 1, 77, float("inf")), (n // 4, 100, float("nan")),
+           (n // 4, 5, float("inf"))]
+    if weights == "first_alone":                                       # the others' weights are 2^-400 of the first token's
+        q, k = torch.zeros_like(q), torch.zeros_like(k)
+        q[..., 0], k[..., 0], k[0, :, 0] = 40.0, -40.0, 40.0
+        if n > 4:
+            k[1, :, 0], bad[0] = 40.0, (2, 5, float("inf"))
+    elif weights == "context_alone":                                   # and here the context's largest scores are far above
+        q, k = q * 60.0, k * 0.0
+    q, k = q.bfloat16(), k.bfloat16()
+    want = torch.zeros(c.T, 128, dtype=torch.float64, device=DEV)
+    with Ctx(Hq, Hkv) as ctx:
+        outs = []
+        for put in (False, True):
+            for (t, col), value in {(t, col): value for t, col, value in bad}.items() if put else ():
+                v[t, last, col] = value
+                want[t:n, col] += value
+            out = torch.empty(c.T, Hq, 128, dtype=torch.bfloat16, device=DEV)
+            cb.confspec_op_kv4_attention(ctx, c.kv, c.batch, 0, q, k, v, out, c.scratch(ctx))
+            outs.append(out.double())
+        torch.cuda.synchronize()
+    want = want[:, None].expand(-1, Hq, -1).clone()
+    want[:, :last * (Hq // Hkv)] = 0.0
+    plain = want == 0.0
+    assert torch.equal(outs[1][plain], outs[0][plain]) and bool(torch.isfinite(outs[0]).all())
+    assert torch.equal(torch.isnan(outs[1]), torch.isnan(want))
+    sure = torch.isinf(want)
+    assert torch.equal(outs[1][sure], want[sure])
