@@ -174,26 +174,27 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
 __device__ __forceinline__ float param_s(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p & 0xffff))); }
 __device__ __forceinline__ float param_z(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p >> 16))); }
 
-// Eight heads of a token a workgroup, four at a time: a wavefront has a head's key and value row, a thread half a word of it, so that
+// Eight heads of a token a workgroup at a time, n_split workgroups per token, four heads at once: a wavefront has a head's key and value row, a thread half a word of it, so that
 // a wavefront's stores are 512 consecutive bytes twice.  Bound by what it writes: 4096 tokens, 8 heads: 10.9 us for 38 MB (3.5 TB/s).
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, float *__restrict__ k, float *__restrict__ v) {
-    const int t = blockIdx.x / n_split, lane = threadIdx.x & 63, h0 = blockIdx.x % n_split * 8 + (threadIdx.x >> 6);
+    const int t = blockIdx.x / n_split, lane = threadIdx.x & 63, first = blockIdx.x % n_split * 8 + (threadIdx.x >> 6);
     const int trace = trace_of(b.cu, b.B, t, lane);
     const int row = min(max(b.plens[trace], 0), b.max_L) + min(max(t - b.cu[trace], 0), b.T - 1), slot = row & 15;
     const int is_v = lane >> 5, d = (lane & 31) * 4;
     const uint8_t *pages = page_of(b, trace, row, 0);
+    for (int h0 = first; h0 < b.Hkv; h0 += 8 * n_split)
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int h = h0 + 4 * u;
-        if (h >= b.Hkv) continue;
-        const uint8_t *page = pages + (size_t)h * KV4_PAGE;
-        const unsigned w = *(const unsigned *)(page + (is_v ? v_word(slot, d & ~7) : k_word(slot, d & ~7)));
-        const unsigned p = *(const unsigned *)(page + (is_v ? KV4_VP : KV4_KP) + slot * 4);
-        float x[4];
+        for (int u = 0; u < 2; ++u) {
+            const int h = h0 + 4 * u;
+            if (h >= b.Hkv) continue;
+            const uint8_t *page = pages + (size_t)h * KV4_PAGE;
+            const unsigned w = *(const unsigned *)(page + (is_v ? v_word(slot, d & ~7) : k_word(slot, d & ~7)));
+            const unsigned p = *(const unsigned *)(page + (is_v ? KV4_VP : KV4_KP) + slot * 4);
+            float x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = fmaf(param_s(p), (float)((w >> (is_v ? 4 * ((d & 4) + e) : k_shift((d & 4) + e))) & 15), param_z(p));
-        *(float4 *)((is_v ? v : k) + ((size_t)t * b.Hkv + h) * 128 + d) = make_float4(x[0], x[1], x[2], x[3]);
-    }
+            for (int e = 0; e < 4; ++e) x[e] = fmaf(param_s(p), (float)((w >> (is_v ? 4 * ((d & 4) + e) : k_shift((d & 4) + e))) & 15), param_z(p));
+            *(float4 *)((is_v ? v : k) + ((size_t)t * b.Hkv + h) * 128 + d) = make_float4(x[0], x[1], x[2], x[3]);
+        }
 }
 
 // ---- attention ----
@@ -958,7 +959,8 @@ hipError_t launch_kv4_append(const Kv4Append &a, hipStream_t s) {
 }
 
 hipError_t launch_kv4_read(const Kv4Batch &b, float *k, float *v, hipStream_t s) {
-    const int n_split = (b.Hkv + 7) / 8;
+    // (a workgroup for every eight heads, while a launch has less than 2^32 threads)
+    const int n_split = std::min((b.Hkv + 7) / 8, std::max(1, ((1 << 24) - 1) / b.T));
     kv4_read_kernel<<<(unsigned)b.T * n_split, 256, 0, s>>>(b, n_split, k, v);
     return hipGetLastError();
 }

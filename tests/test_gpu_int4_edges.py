@@ -185,3 +185,30 @@ def test_attention_infinite_values_of_tokens_seen(Hq, Hkv, L, S, weights):
     assert torch.equal(torch.isnan(outs[1]), torch.isnan(want))
     sure = torch.isinf(want)
     assert torch.equal(outs[1][sure], want[sure])
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# the largest calls, and what lies behind the buffers
+# ---------------------------------------------------------------------------------------------------------------------
+def test_read_of_the_largest_batch():
+    """2^22 tokens of 25 heads, whose rows lie in two pages over and over."""
+    T, Hkv = 1 << 22, 25
+    if torch.cuda.mem_get_info()[0] < 125e9:
+        pytest.skip("needs 125 GB of free device memory")
+    pages = R.random_pages(_gen(56), 1, 2, Hkv, DEV)
+    cu, lens = np.asarray([0, T], dtype=np.int32), np.asarray([0], dtype=np.int32)
+    table = (torch.arange(T // 16, device=DEV, dtype=torch.int32) % 2).view(1, -1).contiguous()
+    d = [torch.from_numpy(cu).to(DEV), torch.from_numpy(lens).to(DEV), torch.zeros(T, dtype=torch.int32, device=DEV)]
+    kv = cb.make_kv4(pages, table, 2, 16, T // 16)
+    batch, keep = cb.make_batch(d[2], d[0], d[1], cu, lens)
+    k, v = (torch.empty(T, Hkv, 128, device=DEV) for _ in range(2))
+    k[-1] = v[-1] = float("nan")
+    with Ctx(Hkv, Hkv) as ctx:
+        cb.confspec_op_kv4_read(ctx, kv, batch, 0, k, v)
+        torch.cuda.synchronize()
+    for got, (codes, s, z) in zip((k, v), R.read_pages(pages[0].reshape(-1, R.PAGE))):
+        want = (z[..., None] + s[..., None] * codes).float().view(2, Hkv, 16, 128).transpose(1, 2).reshape(32, Hkv, 128)
+        for part in got.view(-1, 32, Hkv, 128).split(1 << 13):
+            assert bool((part == want).all())
+    del k, v, got, part
+    torch.cuda.empty_cache()
