@@ -88,7 +88,7 @@ int confspec_op_kv4_attention_scratch_bytes(const confspec_ctx *ctx, const confs
 #define CONFSPEC_W4_MAX_ROWS 128
 
 /* Bytes confspec_w4_pack writes for an [N, K] matrix; 0 where the shape is not supported (N % 16 != 0, group not 32, 64
- * or 128, K % group != 0, K above 2^22, more than 2^34 elements). */
+ * or 128, K % group != 0, K above 2^22, more than 2^34 elements with K rounded up to a multiple of 128). */
 size_t confspec_w4_bytes(int32_t N, int32_t K, int32_t group);
 
 /* Lays a quantised matrix out for confspec_op_w4_gemm, once per matrix.

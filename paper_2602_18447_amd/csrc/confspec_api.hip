@@ -1424,7 +1424,7 @@ int confspec_op_kv4_attention(confspec_ctx *ctx, const confspec_kv4 *kv, const c
 size_t confspec_w4_bytes(int32_t N, int32_t K, int32_t group) {
     if (N < 16 || N % 16 || K < 1 || K > cs::W4_MAX_K || (group != 32 && group != 64 && group != 128) || K % group) return 0;
     const int64_t records = (int64_t)(N / 16) * cs::w4_kblocks(K);
-    return records > INT32_MAX / 256 ? 0 : (size_t)records * cs::w4_record(group);      // (a grid of one workgroup of 256 a record)
+    return records > 1 << 23 ? 0 : (size_t)records * cs::w4_record(group);      // (confspec_w4_pack's grid: one workgroup of 256 a record)
 }
 
 int confspec_w4_pack(confspec_ctx *ctx, const void *dev_codes, const void *dev_scales, const void *dev_zeros, int32_t N,

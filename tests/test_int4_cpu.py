@@ -199,3 +199,13 @@ def test_attention_scratch_stays_small(Hq, Hkv):
         batch, keep = cb.make_batch(d, d, d, cu, L)
         assert cb.confspec_op_kv4_attention_scratch_bytes(ctx, batch) <= 2 * 2049 * 32 * 130 * 4, (B, L.max(), S.max())
     cb.confspec_destroy(ctx)
+
+
+def test_weight_sizes_up_to_the_largest():
+    """2^34 elements, K rounded up to whole records, and no more."""
+    for N, K, group in ((1 << 17, 1 << 17, 128), (1 << 12, 1 << 22, 64), (1 << 27, 128, 32), (1 << 27, 32, 32), (1 << 17, (1 << 17) - 64, 64)):
+        records = (N // 16) * ((K + 127) // 128)
+        assert records == 1 << 23
+        assert cb.confspec_w4_bytes(N, K, group) == records * (1024 + 64 * (128 // group))
+        assert cb.confspec_w4_bytes(N + 16, K, group) == 0
+    assert cb.confspec_w4_bytes(16, (1 << 22) + 128, 128) == 0
