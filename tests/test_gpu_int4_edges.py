@@ -212,3 +212,44 @@ def test_read_of_the_largest_batch():
             assert bool((part == want).all())
     del k, v, got, part
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("Hq, Hkv, L, S", [(12, 2, (2048,), (1,)), (12, 2, (3000, 70, 900), (1, 5, 3)), (40, 8, (4000,) * 9, (1,) * 9), (6, 1, (9000, 17), (150, 3)), (34, 2, (70,) * 12, tuple(range(30, 54, 2)))])
+def test_nothing_is_written_behind_the_buffers(Hq, Hkv, L, S):
+    """Scratch of exactly the size asked for and every output, with bytes behind them that stay as they were."""
+    gen = _gen(57)
+    c = Cache(gen, Hkv, L, S)
+    width = (Hq + 2 * Hkv) * 128
+    qkv = torch.randn(c.T, width, generator=gen, device=DEV)
+    guard = 4096
+
+    def room(n_bytes):
+        return torch.full((n_bytes + guard,), 0xA5, dtype=torch.uint8, device=DEV)
+
+    rows = c.T * 128
+    with Ctx(Hq, Hkv) as ctx:
+        need = cb.confspec_op_kv4_attention_scratch_bytes(ctx, c.batch)
+        sizes = dict(q=2 * rows * Hq, k=2 * rows * Hkv, v=2 * rows * Hkv, out=2 * rows * Hq, kr=4 * rows * Hkv, vr=4 * rows * Hkv, scratch=need)
+        buf = {name: room(n) for name, n in sizes.items()}
+        cb.confspec_op_kv4_append(ctx, c.kv, c.batch, 0, qkv, None, None, buf["q"], buf["k"], buf["v"], qkv_stride=width)
+        cb.confspec_op_kv4_read(ctx, c.kv, c.batch, 0, buf["kr"], buf["vr"])
+        cb.confspec_op_kv4_attention(ctx, c.kv, c.batch, 0, buf["q"], buf["k"], buf["v"], buf["out"], buf["scratch"][:need] if need else None)
+        torch.cuda.synchronize()
+    for name, n in sizes.items():
+        assert bool((buf[name][n:] == 0xA5).all()), name
+    q, k, v = (buf[name][:sizes[name]].view(torch.bfloat16).view(c.T, -1, 128) for name in ("q", "k", "v"))
+    ref, tol = R.attention(c.pages[0], c.table, q, k, v, c.cu, c.lens, Hq, Hkv)
+    got = buf["out"][:sizes["out"]].view(torch.bfloat16).view(c.T, Hq * 128).double()
+    assert bool(((got - ref).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("N, K, group, gate_up", [(16, 32, 32, False), (48, 416, 32, True), (144, 1600, 64, False), (272, 640, 128, True)])
+def test_pack_writes_its_bytes_and_no_other(N, K, group, gate_up):
+    codes, s, z, _ = R.w4_quantise_case(_gen(58), N, K, group, DEV)
+    n = cb.confspec_w4_bytes(N, K, group)
+    first, second = (torch.full((n + 4096,), fill, dtype=torch.uint8, device=DEV) for fill in (0x00, 0xFF))
+    with Ctx() as ctx:
+        for dst in (first, second):
+            cb.confspec_w4_pack(ctx, codes, s, z, N, K, group, dst[:n], gate_up=gate_up)
+    assert torch.equal(first[:n], second[:n])
+    assert bool((first[n:] == 0x00).all()) and bool((second[n:] == 0xFF).all())
