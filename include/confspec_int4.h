@@ -11,9 +11,11 @@
  *
  * Same conventions as confspec.h: dev pointers are caller-owned device memory, nothing is allocated, nothing
  * synchronises, every check that host-visible arguments allow is made before the first launch.  The calls can be
- * captured into HIP graphs; calls on different streams may run at the same time as long as their outputs, scratch
- * and written cache rows differ.  Outputs overlap no other operand unless a function says so.  All of them need a bf16
- * context (head_dim 128); other contexts get CONFSPEC_E_UNSUPPORTED.
+ * captured into HIP graphs: a graph keeps the host lengths and counts of its capture (launches and pieces come from them),
+ * and the device arrays have to hold the same ones at every replay; block tables, cache and operands may change.  Calls on
+ * different streams may run at the same time as long as their outputs, scratch and written cache rows differ.  Outputs
+ * overlap no other operand unless a function says so.  All of them need a bf16 context (head_dim 128); other contexts get
+ * CONFSPEC_E_UNSUPPORTED.
  */
 #ifndef CONFSPEC_INT4_H
 #define CONFSPEC_INT4_H
@@ -73,8 +75,9 @@ int confspec_op_kv4_read(confspec_ctx *ctx, const confspec_kv4 *kv, const confsp
  *                  not be kept between calls, but two calls that may run at the same time need one each (NULL is fine
  *                  where the need is 0)
  * Numerics: q (below 2^116 in magnitude; taken as halves times a power of two of its row) and codes enter the score product
- * exactly; scores, softmax statistics and sums are fp32; probabilities times the value row's s are rounded to IEEE half for
- * the cached rows, carried as two bf16 terms for the suffix.  Suffix values are below 2^90 in magnitude, or no finite numbers: a weight
+ * exactly, but for elements of q 2^-27 times their row's largest, which lose what is below 2^-38 of it; scores, softmax
+ * statistics and sums are fp32; probabilities times the value row's s are rounded to IEEE half for the cached rows, carried
+ * as two bf16 terms for the suffix.  Suffix values are below 2^90 in magnitude, or no finite numbers: a weight
  * is positive, so that an infinity makes its column infinite, and a NaN or infinities of both signs NaN, in the rows that see the
  * token, and in no other. */
 int confspec_op_kv4_attention(confspec_ctx *ctx, const confspec_kv4 *kv, const confspec_batch *batch, int32_t layer,
@@ -100,7 +103,9 @@ int confspec_w4_pack(confspec_ctx *ctx, const void *dev_codes, const void *dev_s
                      int32_t K, int32_t group, int32_t gate_up, void *dev_dst, size_t dst_bytes, confspec_stream stream);
 
 /* out = A . W^T with an epilogue of confspec_ops.h: A bf16 [M, K] row-major, 1 <= M <= CONFSPEC_W4_MAX_ROWS, W as
- * confspec_w4_pack wrote it (same N, K, group).
+ * confspec_w4_pack wrote it (same N, K, group).  Nothing in the packed bytes says how they were packed: with another group
+ * or shape the result is wrong, and where that has more confspec_w4_bytes, bytes behind the matrix are read; a matrix
+ * packed with gate_up = 1 goes with the SwiGLU epilogue, and only with it.
  *   CONFSPEC_EPI_STORE_F32 : out fp32 [M, N]
  *   CONFSPEC_EPI_RESID_F32 : out fp32 [M, N] = dev_residual + A . W^T (dev_residual may be dev_out: in place)
  *   CONFSPEC_EPI_SWIGLU    : W packed with gate_up = 1; out bf16 [M, N / 2] = silu(gate) * up

@@ -174,8 +174,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Append a, int n_spli
 __device__ __forceinline__ float param_s(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p & 0xffff))); }
 __device__ __forceinline__ float param_z(unsigned p) { return __half2float(__ushort_as_half((unsigned short)(p >> 16))); }
 
-// Eight heads of a token a workgroup at a time, n_split workgroups per token, four heads at once: a wavefront has a head's key and value row, a thread half a word of it, so that
-// a wavefront's stores are 512 consecutive bytes twice.  Bound by what it writes: 4096 tokens, 8 heads: 10.9 us for 38 MB (3.5 TB/s).
+// Eight heads of a token a workgroup at a time, n_split workgroups per token, four heads at once: a wavefront has a head's key and value
+// row, a thread half a word of it, so that a wavefront's stores are 512 consecutive bytes twice.  Bound by what it writes: 4096 tokens, 8 heads: 10.9 us for 38 MB (3.5 TB/s).
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, float *__restrict__ k, float *__restrict__ v) {
     const int t = blockIdx.x / n_split, lane = threadIdx.x & 63, first = blockIdx.x % n_split * 8 + (threadIdx.x >> 6);
     const int trace = trace_of(b.cu, b.B, t, lane);
@@ -211,6 +211,9 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, 
 //    a page's value codes lie in memory such that a lane's 16 bytes are those four tokens of eight columns.  Codes enter as
 //    the keys' do, the probability as the half p s; z is added to the row's sum.  The lane has 32 columns of its one query row,
 //    so scaling, sums and output need nothing of other lanes.
+//    The rounding of p s moves what a row adds by less than p 15 2^-11 s, where the row's own step is p s; a second half for what it drops
+//    would double the products.  Measured (48 traces of 2000 to 16384 tokens): outputs are 1.75e-3 (rms) from 64 bits, with probabilities in fp32
+//    1.66e-3, most of either the rounding to bf16.
 //  * The running reference M of a row is a bound of score + exponent of s (p s is what must fit a half).  A chunk takes it as it is and
 //    looks at the halves that come out; only where one has grown too large, M is raised, what was summed scaled and the chunk's
 //    probabilities taken again.
@@ -901,7 +904,11 @@ struct Launch4 {
     int rows_log2() const { return __builtin_ctz(16 * nq * wr); }
     size_t record_rows() const { return (size_t)plan.n_records << rows_log2(); }
 };
-// Pieces are of 32 chunks at least.  With eight wavefronts one workgroup fits a CU, and what does not fit at once waits for a whole item: as
+// Pieces are of 32 chunks at least: smaller ones bring the join, and its launch, to contexts that one piece finishes sooner.  Measured, us, with at
+// least 16, 32 and 64 chunks: one token of 12 heads on 2, on 512 keys 9.8, 7.0, 7.0; 1024: 9.8, 10.3, 8.6; 2048: 10.9, 11.2, 11.9; 4096: 11.2,
+// 11.9, 13.1; 8192: 12.4, 13.0, 14.2;  16 traces of one, 40 heads on 8, on 512: 10.6, 7.4, 7.4; 1024: 11.6, 11.4, 9.3; 8192: 30.3, 29.8, 30.7;
+// 32 traces of 20 to 100 tokens on 100 to 900: 37.6, 27.3, 27.2.
+// With eight wavefronts one workgroup fits a CU, and what does not fit at once waits for a whole item: as
 // few items as there are CUs (one token on 16384 keys, 12 heads on 2: 13.7 us; in pieces of a power of two of chunks, which leave some CUs
 // without, 18).  With four, two or three fit, and more items even out (16 traces of 32 to 256 tokens: 135 us, with 1024 items 141).
 constexpr int ATT_MIN_CHUNKS = 32;

@@ -73,8 +73,9 @@ __device__ __forceinline__ bf16x8 code_operand(unsigned w, CodeBits b) {
 //    as the halves they are: sum += s (part - z sum(a)).
 // Bound by the bytes of W while rows are few; every workgroup reads its rows of A from L2.  N = 55296, K = 5120, groups of 128, one row: 24.8
 // us (6.1 TB/s, the weights come from the last-level cache; 30 with other weights each time, 5.0).  N = 5120, K = 27648, groups of 64, 8
-// rows: 19.2 us (4.2 TB/s; 24.2), as its 160 tiles of 32 rows leave 96 CUs without.  72 rows, N = 7168, K = 5120, groups of 32: 22.4 us,
-// bound by the vector pipe (8 multiply-adds a group and 16 x 16 results, 128 to unpack 64 x 128 codes) and its turns with the matrix pipe.
+// rows: 19.2 us (4.2 TB/s; 24.2), as its 160 tiles of 32 rows leave 96 CUs without.  72 rows, N = 7168, K = 5120, groups of 32: 22.4 us, in
+// which no pipe is full (vector 43 %, matrix 15 %, wavefronts wait a third of their time): a block of k is load, stage, unpack and product in
+// turn, with no load in flight meanwhile, every wavefront stages rows of A of its own, and each tile of W reads all of A again.
 template <int NG>
 struct Params;
 template <> struct Params<1> { typedef unsigned T; static __device__ unsigned get(T p, int) { return p; } };
@@ -316,8 +317,8 @@ hipError_t launch_w4_pack(const uint8_t *codes, const __half *scales, const __ha
 // Measured (us) for 1x1, 1x2 and 2x2 with 8 wavefronts, at so many tiles of 16 x 16: 34 (25 rows, N = 272, K = 17824, groups of 32): 12.7,
 // 17.1, 28.3;  256 (20, 2048, 4096, 128): 5.5, 6.0, 8.0;  288 (40, 1536, 4096, 64): 7.8, 6.4, 8.2;  512 (20, 4096, 2048, 64): 6.0, 5.3, 6.0;
 // 640 (30, 5120, 5120, 128): 16.7, 12.3, 10.9;  768 (128, 1536, 8960, 128): 21.5, 17.3, 14.9.
-// Others are bound by the vector and matrix pipes: the tile with the least of w4_cost, in rounds of 256 workgroups.  Measured (us)
-// for 2x2, 2x4, 3x2, 3x4, 4x4 tiles of 16: 72 rows, N = 7168, K = 5120, groups of 128: 21.0, 19.9, 19.8, 16.2, 19.8;  48, 5120, 5120, 64:
+// Others take what a wavefront does in a block, one thing after the other: the tile with the least of w4_cost, in rounds of 256 workgroups.  Measured (us)
+// for 2x2, 2x4, 3x2, 3x4, 4x4 tiles of 16 (4x4 with groups of 32 keeps one register in memory): 72 rows, N = 7168, K = 5120, groups of 128: 21.0, 19.9, 19.8, 16.2, 19.8;  48, 5120, 5120, 64:
 // 15.6, 14.4, 13.8, 17.9, -;  128, 1536, 8960, 128: 14.7, 18.3, 17.3, -, -;  128, 55296, 5120, 128: 166, 131, -, 139, 120.
 struct W4Tile { int mt, nt, W; };
 
