@@ -436,6 +436,14 @@ __device__ __forceinline__ void cached_chunk(Rows4<NQ> &R, const Chunk4 &c, int 
     }
 }
 
+// Eight values: a full exponent carries into its sign's place.
+__device__ __forceinline__ unsigned exponent_full(u32x4 w) {
+    unsigned any = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) any |= (w[e] & 0x7fff7fffu) + 0x00800080u;
+    return any;
+}
+
 // Adds the values of tokens j_begin .. j_end - 1 that are not finite numbers to the rows that see them.  A probability is positive,
 // so that an infinity or NaN is what its column becomes, whatever the probability.
 template <int NQ>
@@ -459,9 +467,9 @@ __device__ __forceinline__ void add_not_finite(Rows4<NQ> &R, const bf16 *v, unsi
 
 // Columns that came out as NaN, from the values of the tokens that were attended to: the two terms of a probability may have both
 // signs or be 0, so that an infinity ends as NaN where the definition has an infinity.  (A NaN of the scores or of the cache is in R.l or
-// R.zs too, and stays.)
+// R.zs too, and stays.)  One infinity among the first of 4096 tokens, 40 heads on 8: 0.76 ms, 0.45 without; a trace of NaN does not come here.
 template <int NQ>
-__device__ __forceinline__ void settle_not_finite(Rows4<NQ> &R, const bf16 *v, unsigned stride, int j0, int j_step, int j_end, int S, const int (&tok)[NQ], int g) {
+__device__ __forceinline__ void settle_not_finite(Rows4<NQ> &R, const bf16 *v, unsigned stride, int j0, int j_step, int j_end, int S, const int (&tok)[NQ], int n15, int g) {
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -471,7 +479,12 @@ __device__ __forceinline__ void settle_not_finite(Rows4<NQ> &R, const bf16 *v, u
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll 1
-    for (; j0 < j_end; j0 += j_step) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
+    for (; j0 < j_end; j0 += j_step) {
+        unsigned any = 0;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) any |= exponent_full(*(const u32x4 *)(v + (uint64_t)(unsigned)min(j0 + 16 * (t >> 2) + 4 * g + (t & 3), S - 1) * stride + 8 * n15));
+        if (__any((any & 0x80008000u) != 0u)) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
+    }
 }
 
 // Suffix tokens, 32 from j0 on, then from j0 + j_step, below j_end; k, v point at the trace's first token and the head, rows are `stride`
@@ -526,8 +539,7 @@ __device__ __forceinline__ void attend_suffix(Rows4<NQ> &R, bool &big, const bf1
                 for (int n = 0; n < NQ; ++n)
                     if (j > tok[n]) sc[n][t >> 2][t & 3] = -INFINITY;
                 if (j >= S) vw[t] = u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) any |= (vw[t][e] & 0x7fff7fffu) + 0x00800080u;      // a full exponent carries into the sign's place
+                any |= exponent_full(vw[t]);
             }
             bad = __any((any & 0x80008000u) != 0u);
             if (bad)
@@ -607,14 +619,17 @@ __device__ __forceinline__ void attend_suffix(Rows4<NQ> &R, bool &big, const bf1
         if (bad) add_not_finite<NQ>(R, v, stride, j0, min(j0 + 32, S), tok, g);
     }
     if (whole) {
-        float all = 0.f;
+        bool lost = false;            // (where scores are NaN, so is the sum of the probabilities, and nothing can be settled)
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
+        for (int n = 0; n < NQ; ++n) {
+            float all = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) all += R.o[n][j][r];
-        if (__any(all != all)) settle_not_finite<NQ>(R, v, stride, j_first, j_step, j_end, S, tok, g);
+            lost |= all != all && R.l[n] == R.l[n];
+        }
+        if (__any(lost)) settle_not_finite<NQ>(R, v, stride, j_first, j_step, j_end, S, tok, n15, g);
     }
 }
 
