@@ -211,9 +211,10 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Batch b, int n_split, 
 //    a page's value codes lie in memory such that a lane's 16 bytes are those four tokens of eight columns.  Codes enter as
 //    the keys' do, the probability as the half p s; z is added to the row's sum.  The lane has 32 columns of its one query row,
 //    so scaling, sums and output need nothing of other lanes.
-//    The rounding of p s moves what a row adds by less than p 15 2^-11 s, where the row's own step is p s; a second half for what it drops
-//    would double the products.  Measured (48 traces of 2000 to 16384 tokens): outputs are 1.75e-3 (rms) from 64 bits, with probabilities in fp32
-//    1.66e-3, most of either the rounding to bf16.
+//    The rounding of p s moves what a row adds by less than p 15 2^-11 s, where the row's own step is p s.  Measured (48 traces of 2000 to 16384
+//    tokens; 16 of steps of 32 to 256): outputs are 1.75e-3, 1.73e-3 (rms) from 64 bits, with probabilities in fp32 1.66e-3, most of it the
+//    rounding to bf16.  A second half for what the first drops brings 1.66e-3, in 100 for 99 us and 157 for 135; codes counted from 8 (the sum
+//    of the halves by one more product a row) 1.67e-3, in 99 and 138.5: not worth it beside steps of a fifteenth of a row's range.
 //  * The running reference M of a row is a bound of score + exponent of s (p s is what must fit a half).  A chunk takes it as it is and
 //    looks at the halves that come out; only where one has grown too large, M is raised, what was summed scaled and the chunk's
 //    probabilities taken again.
